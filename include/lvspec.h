@@ -58,10 +58,13 @@ typedef enum {
 /* Bits of the device status word (lvspec_device_status). */
 #define LVSPEC_DEV_WAIT_EXPIRED 0x1u /* a bounded wait gave up; that call's results are invalid */
 #define LVSPEC_DEV_NAN_LOGIT    0x2u /* a NaN logit was seen (it was ranked as -inf) */
+#define LVSPEC_DEV_REFUSED      0x4u /* lvspec_plan_pages refused a request */
+#define LVSPEC_DEV_BAD_LENGTH   0x8u /* a length on the device was outside its range; the sequence counted as empty */
 
 #define LVSPEC_MAX_BATCH 128   /* sequences per call */
 #define LVSPEC_MAX_ROWS  128   /* gamma * (Hq / Hkv): query rows sharing one KV head */
 #define LVSPEC_MAX_GAMMA 64    /* draft tokens per sequence */
+#define LVSPEC_MAX_REQUESTS 1024 /* requests per lvspec_plan_pages call */
 
 typedef struct lvspec_ctx lvspec_ctx_t; /* opaque */
 
@@ -374,6 +377,136 @@ lvspec_status_t lvspec_verify_attention_fp8(lvspec_ctx_t *ctx, const lvspec_attn
                                             const float *k_scale, const float *v_scale,
                                             const int32_t *kv_len, const int32_t *visual_span,
                                             void *out, float *visual_mass);
+
+/* ---- a decoding step on a paged fp8 cache -----------------------------------------
+ *
+ * A serving engine's cache: pages of fixed size in pools that all sequences share, K and V in
+ * E4M3 (see lvspec_verify_attention_fp8) with one scale for each block of positions and KV head,
+ * lengths on the device.  A step runs, on one stream and without the host in between:
+ *
+ *   lvspec_plan_pages                 pages for the new tokens, block table, slot map
+ *   lvspec_append_paged_fp8           (each layer) the new K and V rows into their slots
+ *   lvspec_verify_attention_paged_fp8 (each layer) the attention
+ *   lvspec_loose_accept_emit          the rule; its new_kv_len are the next step's lengths
+ *
+ * All three calls read their lengths, tables and maps on the device, so a captured step follows
+ * lengths that change from replay to replay.
+ *
+ * Layout of the pools: element (page, head, position in the page, channel) of K sits at
+ * k_pool + page * page_stride + head * head_stride + position * position_stride + channel, V
+ * likewise with the same strides.  All three strides 0: the dense [n_pages, Hkv, page_size, D].
+ * Otherwise they are positive multiples of 16 below 2^38, the position stride at least head_dim;
+ * [n_pages, page_size, Hkv, D] is {page_size * Hkv * D, D, Hkv * D}; K and V interleaved in one
+ * buffer [n_pages, 2, Hkv, page_size, D] is {2 * Hkv * page_size * D, page_size * D, D} with
+ * v_pool = k_pool + Hkv * page_size * D.  Elements must not overlap.
+ *   k_scale, v_scale  device, fp32  [n_pages, Hkv, page_size / scale_block]
+ * A cache value is code * scale. */
+typedef struct {
+    int32_t page_size;       /* 16, 32 or 64, or a multiple of 128 */
+    int32_t n_pages;         /* pages in a pool; n_pages * page_size below 2^31 */
+    int32_t scale_block;     /* 16, 32, 64 or 128 positions per scale; divides page_size */
+    int32_t reserved;        /* 0 */
+    int64_t page_stride;     /* bytes (= elements); all three 0: dense */
+    int64_t head_stride;
+    int64_t position_stride;
+} lvspec_paged_fp8_t;
+
+/* Page tables of a step.  Request b holds kv_len[b] positions in the first pages_held[b] pages
+ * of its row of the block table and asks for n_new[b] more positions:
+ *
+ *   need_b  = max(0, ceil((kv_len[b] + n_new[b]) / page_size) - pages_held[b])
+ *   taken   from the end of the free list, free_pages[n_free - 1] first, for the requests in order;
+ *           they become entries pages_held[b].. of the request's row
+ *   slot of new token i of request b = page * page_size + offset of position kv_len[b] + i
+ *
+ * The new tokens of all requests sit one behind the other (a ragged batch's rows): those of
+ * request b from token_start[b] on.  Slots that no token has, up to max_new, are -1.  (After a
+ * step that rejected draft tokens kv_len is shorter than what the pages hold: nothing is
+ * given back, the next step fills them.  A request that ends gives its pages back by putting its
+ * row's first pages_held entries at the end of the free list.)
+ *
+ *   kv_len, n_new, pages_held  device, int32 [B]       B 1..LVSPEC_MAX_REQUESTS
+ *   n_free          device, int32 [1]
+ *   free_pages      device, int32 [n_pages]
+ *   block_table     device, int32 [B, pages_per_seq]   (new entries written)
+ *   new_kv_len      device, int32 [B]    (written) kv_len + n_new; may be kv_len
+ *   new_pages_held  device, int32 [B]    (written) may be pages_held
+ *   new_n_free      device, int32 [1]    (written) may be n_free
+ *   token_start     device, int32 [B + 1] (written) sums of n_new; the last is their total
+ *   slot_map        device, int32 [max_new] (written)
+ *
+ * A request is refused, alone, if its lengths or page count are negative or beyond pages_per_seq,
+ * if its tokens end beyond max_new, or if the pages that the requests up to it need are more than
+ * are free: it keeps its lengths, its slots are -1, and LVSPEC_DEV_REFUSED is raised.  Requests
+ * that need no page are not refused for want of them.  (A negative n_new counts as 0 in token_start.)  A
+ * position on a page outside 0..n_pages-1 has slot -1.
+ * Arrays that are written must not overlap others except as said above.
+ * Errors: INVALID_ARG (null or misaligned pointers, sizes out of range, max_new < 0,
+ * n_pages * page_size or pages_per_seq * page_size beyond 2^31 - 1); CUDA. */
+lvspec_status_t lvspec_plan_pages(lvspec_ctx_t *ctx, int32_t batch, int32_t page_size, int32_t pages_per_seq, int32_t n_pages,
+                                  int32_t max_new, const int32_t *kv_len, const int32_t *n_new, const int32_t *pages_held,
+                                  const int32_t *n_free, const int32_t *free_pages, int32_t *block_table, int32_t *new_kv_len,
+                                  int32_t *new_pages_held, int32_t *new_n_free, int32_t *token_start, int32_t *slot_map);
+
+/* New K and V rows into a paged fp8 cache.  For the new rows that fall into one block of
+ * scale_block positions, of one KV head:
+ *
+ *   a     = largest finite magnitude among them
+ *   scale = 2^ceil(log2(a / 448)), the smallest power of two with a / scale <= 448; within 2^-100..2^119
+ *           (2^-100 if a = 0).  If the block has positions before the first of the new rows,
+ *           scale = the larger of that and the block's scale, and the codes of those
+ *           positions become e4m3(decode(code) * old scale / scale) if it grew
+ *   code  = e4m3(x / scale): to nearest, ties to even; infinities become +-448, NaN stays NaN
+ *
+ * Powers of two cost nothing in a floating-point format, and a block whose scale grows while its
+ * positions come in one by one keeps its normal codes' digits.  What lies behind the new rows in a block is left as it is.
+ *
+ *   k, v        device, bf16  rows [Hkv, D] of n_tokens tokens, k_token_stride / v_token_stride
+ *               elements apart (multiples of 8, at least Hkv * D): a slice of a fused
+ *               projection's output can be passed as it is
+ *   slot_map    device, int32 [n_tokens]: from lvspec_plan_pages; a slot outside
+ *               0..n_pages * page_size - 1 means the token has none
+ *   pools and scales (written) as above
+ *
+ * Tokens of one block must be neighbours in slot_map (as lvspec_plan_pages makes them) and slots distinct; otherwise
+ * what the blocks concerned hold is undefined (nothing else is touched).  n_tokens = 0 does nothing.
+ * Errors: INVALID_ARG (null or misaligned pointers, sizes or strides out of range), UNSUPPORTED
+ * (head_dim other than 64 or 128); CUDA. */
+lvspec_status_t lvspec_append_paged_fp8(lvspec_ctx_t *ctx, int32_t n_tokens, int32_t n_kv_heads, int32_t head_dim,
+                                        const lvspec_paged_fp8_t *cache, const void *k, const void *v, int64_t k_token_stride,
+                                        int64_t v_token_stride, const int32_t *slot_map, void *k_pool, void *v_pool,
+                                        float *k_scale, float *v_scale);
+
+/* lvspec_verify_attention on a paged fp8 cache with a scale per block.  The operation of Eq. 1 as
+ * above, on the cache values k_scale[page, h, block] * decode(code), v likewise, with
+ *
+ *   n_branches   1, or the branches of a draft-token tree as for lvspec_verify_attention_tree
+ *   max_kv_len   host: no sequence is longer, 1..kv_capacity (what work is laid out for)
+ *   block_table  device, int32 [B, kv_capacity / page_size]; only entries of pages that hold
+ *                positions below kv_len[b] are read; positions of an entry outside
+ *                0..n_pages-1 read as zeros
+ *   kv_len       device, int32 [B]: 0..max_kv_len.  0: an empty place of the batch.  Outside that
+ *                range: LVSPEC_DEV_BAD_LENGTH is raised and the sequence counts as empty
+ *   visual_span  device, int32 [B][2]: mass is taken over its positions that the query sees
+ *
+ * A query that sees no position (an empty sequence; kv_len < gamma) gets out = 0 and mass = 0.
+ * shape->n_split must be 0: tiles are shared out on the device, from the lengths.  gamma = 1 is
+ * plain decoding.  Cache contents at and behind kv_len may be anything.
+ * Arithmetic: scores are 8-bit x (q in two E4M3 terms), accumulated in fp32; softmax, its sums and the visual mass are
+ * fp32; the product with V is fp16 x fp16 accumulated in fp32, probabilities in fp16 relative to the
+ * first position a CTA works on: those below 2^-27 of it, times the ratio of the V scales, vanish from `out`.
+ * q loses nothing down to 2^-10 of the largest magnitude among the rows of a KV head.  A NaN code in a draft
+ * slot reaches all queries of its head, also those that do not see it.
+ * Scratch: lvspec_attention_paged_fp8_workspace_bytes (for lvspec_reserve ahead of a capture).
+ * Errors: as lvspec_verify_attention, and INVALID_ARG for an n_split that is not 0, a cache description out of range, kv_capacity not
+ * a whole number of pages, max_kv_len out of range, batch * n_kv_heads * ceil(max_kv_len / 128) beyond 2^30;
+ * UNSUPPORTED for LVSPEC_KERNEL_SIMT. */
+lvspec_status_t lvspec_verify_attention_paged_fp8(lvspec_ctx_t *ctx, const lvspec_attn_shape_t *shape,
+                                                  const lvspec_paged_fp8_t *cache, int32_t n_branches, int32_t max_kv_len,
+                                                  const void *q, const void *k_pool, const void *v_pool, const float *k_scale,
+                                                  const float *v_scale, const int32_t *block_table, const int32_t *kv_len,
+                                                  const int32_t *visual_span, void *out, float *visual_mass);
+size_t lvspec_attention_paged_fp8_workspace_bytes(const lvspec_ctx_t *ctx, const lvspec_attn_shape_t *shape);
 
 /* Same operation on HOST buffers: copies q, the caches, and the results through
  * device staging memory the context owns (grown on demand), on the context's

@@ -21,8 +21,8 @@ LIB_PATH = os.path.join(_HERE, "liblvspec.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
 KERNEL_DEFAULT, KERNEL_SIMT, KERNEL_TCGEN05 = 0, 1, 2
-DEV_WAIT_EXPIRED, DEV_NAN_LOGIT = 0x1, 0x2
-MAX_BATCH, MAX_ROWS, MAX_GAMMA = 128, 128, 64
+DEV_WAIT_EXPIRED, DEV_NAN_LOGIT, DEV_REFUSED, DEV_BAD_LENGTH = 0x1, 0x2, 0x4, 0x8
+MAX_BATCH, MAX_ROWS, MAX_GAMMA, MAX_REQUESTS = 128, 128, 64, 1024
 
 EXPORTS = (
     "lvspec_create", "lvspec_destroy", "lvspec_set_stream", "lvspec_device_status",
@@ -36,7 +36,8 @@ EXPORTS = (
     "lvspec_attention_workspace_bytes", "lvspec_accept_workspace_bytes",
     "lvspec_relevance_workspace_bytes", "lvspec_workspace_capacity", "lvspec_reserve",
     "lvspec_verify_attention_fp8", "lvspec_verify_attention_strided", "lvspec_merge_polls",
-    "lvspec_set_gpu_shared", "lvspec_merge_handed_over",
+    "lvspec_set_gpu_shared", "lvspec_merge_handed_over", "lvspec_plan_pages", "lvspec_append_paged_fp8",
+    "lvspec_verify_attention_paged_fp8", "lvspec_attention_paged_fp8_workspace_bytes",
 )
 
 
@@ -48,6 +49,11 @@ class AttnShape(ctypes.Structure):
 
 class KvStrides(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("position", ctypes.c_int64)]
+
+
+class PagedFp8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("page_size", "n_pages", "scale_block", "reserved")] + \
+               [(n, ctypes.c_int64) for n in ("page_stride", "head_stride", "position_stride")]
 
 
 class Thresholds(ctypes.Structure):
@@ -124,6 +130,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.lvspec_visual_relevance.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i32, vp]
     lib.lvspec_loose_accept_static.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, T, i32, vp,
                                                ctypes.c_char_p, ctypes.c_size_t]
+    PF = ctypes.POINTER(PagedFp8)
+    i64 = ctypes.c_int64
+    lib.lvspec_plan_pages.argtypes = [vp] + [i32] * 5 + [vp] * 11
+    lib.lvspec_append_paged_fp8.argtypes = [vp, i32, i32, i32, PF, vp, vp, i64, i64] + [vp] * 5
+    lib.lvspec_verify_attention_paged_fp8.argtypes = [vp, S, PF, i32, i32] + [vp] * 10
+    lib.lvspec_attention_paged_fp8_workspace_bytes.argtypes = [vp, S]
+    lib.lvspec_attention_paged_fp8_workspace_bytes.restype = sz
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is ctypes.c_int and name not in ("lvspec_attention_splits", "lvspec_attention_splits_fp8"):
@@ -314,6 +327,35 @@ class Context:
             self._h, ctypes.byref(shape), _addr(q), _addr(k_cache), _addr(v_cache), kv_len.ctypes.data,
             int(spans.shape[1]), spans.ctypes.data, _addr(out), _addr(visual_mass)))
 
+    # -- a decoding step on a paged fp8 cache ---------------------------------------------
+    def plan_pages(self, batch, page_size, pages_per_seq, n_pages, max_new, kv_len, n_new, pages_held, n_free,
+                   free_pages, block_table, new_kv_len, new_pages_held, new_n_free, token_start, slot_map) -> None:
+        """All arrays are device int32; new_kv_len, new_pages_held and new_n_free may be their inputs."""
+        self._check(self._lib.lvspec_plan_pages(
+            self._h, int(batch), int(page_size), int(pages_per_seq), int(n_pages), int(max_new), _addr(kv_len), _addr(n_new),
+            _addr(pages_held), _addr(n_free), _addr(free_pages), _addr(block_table), _addr(new_kv_len),
+            _addr(new_pages_held), _addr(new_n_free), _addr(token_start), _addr(slot_map)))
+
+    def append_paged_fp8(self, n_tokens, n_kv_heads, head_dim, cache: PagedFp8, k, v, k_token_stride, v_token_stride,
+                         slot_map, k_pool, v_pool, k_scale, v_scale) -> None:
+        """k, v: device bf16 rows [n_kv_heads, head_dim] per token, the token strides in elements apart;
+        cache: see ``paged_fp8``."""
+        self._check(self._lib.lvspec_append_paged_fp8(
+            self._h, int(n_tokens), int(n_kv_heads), int(head_dim), ctypes.byref(cache), _addr(k), _addr(v), int(k_token_stride),
+            int(v_token_stride), _addr(slot_map), _addr(k_pool), _addr(v_pool), _addr(k_scale), _addr(v_scale)))
+
+    def verify_attention_paged_fp8(self, shape: AttnShape, cache: PagedFp8, q, k_pool, v_pool, k_scale, v_scale, block_table,
+                                   kv_len, visual_span, out, visual_mass, max_kv_len=None, n_branches: int = 1) -> None:
+        """kv_len [B] and visual_span [B, 2] are device int32; no sequence is longer than max_kv_len
+        (default: the block table's capacity)."""
+        self._check(self._lib.lvspec_verify_attention_paged_fp8(
+            self._h, ctypes.byref(shape), ctypes.byref(cache), int(n_branches),
+            shape.kv_capacity if max_kv_len is None else int(max_kv_len), _addr(q), _addr(k_pool), _addr(v_pool), _addr(k_scale),
+            _addr(v_scale), _addr(block_table), _addr(kv_len), _addr(visual_span), _addr(out), _addr(visual_mass)))
+
+    def attention_paged_fp8_workspace_bytes(self, shape: AttnShape) -> int:
+        return int(self._lib.lvspec_attention_paged_fp8_workspace_bytes(self._h, ctypes.byref(shape)))
+
     def select_branch(self, batch, n_branches, accept_len, best_branch, best_len) -> None:
         self._check(self._lib.lvspec_select_branch(self._h, int(batch), int(n_branches), _addr(accept_len),
                                                    _addr(best_branch), _addr(best_len)))
@@ -397,3 +439,8 @@ def available_kernels():
 def attn_shape(batch, gamma, n_q_heads, n_kv_heads, head_dim, kv_capacity, n_split=0,
                kernel=KERNEL_DEFAULT) -> AttnShape:
     return AttnShape(batch, gamma, n_q_heads, n_kv_heads, head_dim, kv_capacity, n_split, kernel)
+
+
+def paged_fp8(page_size, n_pages, scale_block, page_stride=0, head_stride=0, position_stride=0) -> PagedFp8:
+    """Layout of a paged fp8 cache; strides in bytes, all 0: dense [n_pages, Hkv, page_size, D]."""
+    return PagedFp8(page_size, n_pages, scale_block, 0, page_stride, head_stride, position_stride)

@@ -21,6 +21,7 @@ struct lvspec_ctx {
     uint32_t *status = nullptr;       // device status word
     uint32_t *counters = nullptr;     // [LVSPEC_MAX_BATCH] tickets of the acceptance kernel
     uint32_t *rel_counters = nullptr; // [LVSPEC_MAX_BATCH * LVSPEC_MAX_GAMMA] candidate counts of the relevance score
+    uint32_t *plan_ticket = nullptr;  // ticket of the page tables' kernel
     void *scratch = nullptr;          // split partials / argmax partials
     size_t scratch_bytes = 0;
     bool scratch_in_graph = false;    // a call was captured although two waves would not fit: see run_attention
@@ -53,6 +54,7 @@ lvspec_status_t cuda_fail(lvspec_ctx *ctx, const char *what, cudaError_t err)
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Is the context's stream being captured into a CUDA graph right now?  (On the legacy
 // default stream the query itself fails while another stream captures: that too counts.)
@@ -259,11 +261,10 @@ size_t attention_scratch_bytes(int B, int Hkv, int n_split, int M, int D, int ga
            (with_lse ? (size_t)B * gamma * Hq * sizeof(float) : 0);
 }
 
-// Validation shared by the device and host forms.  On success fills seq.
-lvspec_status_t check_attention(lvspec_ctx *ctx, const lvspec_attn_shape_t *s, const void *q,
-                                const void *k, const void *v, const int32_t *kv_len,
-                                const int32_t *span, const void *out, const float *mass,
-                                bool device_ptrs, SeqInfo *seq, int *max_len)
+// Validation of an attention call but for its lengths.
+lvspec_status_t check_attention_shape(lvspec_ctx *ctx, const lvspec_attn_shape_t *s, const void *q,
+                                      const void *k, const void *v, const int32_t *kv_len,
+                                      const int32_t *span, const void *out, const float *mass, bool device_ptrs)
 {
     if (!ctx) return LVSPEC_ERR_INVALID_ARG;
     if (!s || !q || !k || !v || !kv_len || !span || !out || !mass)
@@ -290,6 +291,17 @@ lvspec_status_t check_attention(lvspec_ctx *ctx, const lvspec_attn_shape_t *s, c
     if (device_ptrs && (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) ||
                         (reinterpret_cast<uintptr_t>(mass) & 3u)))
         return fail(ctx, LVSPEC_ERR_INVALID_ARG, "device tensors must be 16-byte aligned");
+    return LVSPEC_OK;
+}
+
+// Validation shared by the device and host forms.  On success fills seq.
+lvspec_status_t check_attention(lvspec_ctx *ctx, const lvspec_attn_shape_t *s, const void *q,
+                                const void *k, const void *v, const int32_t *kv_len,
+                                const int32_t *span, const void *out, const float *mass,
+                                bool device_ptrs, SeqInfo *seq, int *max_len)
+{
+    const lvspec_status_t st = check_attention_shape(ctx, s, q, k, v, kv_len, span, out, mass, device_ptrs);
+    if (st != LVSPEC_OK) return st;
     int mx = 0;
     for (int b = 0; b < s->batch; ++b) {
         const int L = kv_len[b], vs = span[2 * b], ve = span[2 * b + 1];
@@ -316,6 +328,37 @@ struct PagedCache {          // page pools instead of one contiguous cache per s
 struct Fp8Cache {            // E4M3 codes with one scale per (sequence, KV head)
     const float *k_scale = nullptr, *v_scale = nullptr;
 };
+
+// A paged fp8 cache's description, its strides filled in.
+struct PagedFp8Layout {
+    int64_t page = 0, head = 0, position = 0;
+    int block_log2 = 0;
+};
+lvspec_status_t check_paged_fp8(lvspec_ctx *ctx, const lvspec_paged_fp8_t *c, int n_kv_heads, int head_dim, PagedFp8Layout *out)
+{
+    if (!c) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "null argument");
+    if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && (c->page_size < 128 || c->page_size % 128 != 0))
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "page_size must be 16, 32, 64 or a multiple of 128");
+    if (c->n_pages < 1 || (int64_t)c->n_pages * c->page_size > 2147483647ll)
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "n_pages outside 1..2^31 / page_size");
+    out->block_log2 = c->scale_block == 16 ? 4 : c->scale_block == 32 ? 5 : c->scale_block == 64 ? 6 : c->scale_block == 128 ? 7 : 0;
+    if (!out->block_log2 || c->page_size % c->scale_block != 0)
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "scale_block must be 16, 32, 64 or 128 and divide page_size");
+    if (c->reserved != 0) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "reserved must be 0");
+    out->page = c->page_stride;
+    out->head = c->head_stride;
+    out->position = c->position_stride;
+    if (!out->page && !out->head && !out->position) {
+        out->position = head_dim;
+        out->head = (int64_t)c->page_size * head_dim;
+        out->page = n_kv_heads * out->head;
+    }
+    for (const int64_t s : {out->page, out->head, out->position})
+        if (s < 1 || (s & 15) || s >= (int64_t(1) << 38))
+            return fail(ctx, LVSPEC_ERR_INVALID_ARG, "pool strides must be positive multiples of 16 bytes below 2^38");
+    if (out->position < head_dim) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "the position stride must be at least head_dim");
+    return LVSPEC_OK;
+}
 
 constexpr size_t kMergeWordBytes = 8 * kMergeWords;
 static_assert(kMergeCountWord >= 256, "a word per CTA of the widest device");
@@ -593,7 +636,7 @@ lvspec_status_t lvspec_create(lvspec_ctx_t **out, int device)
     ctx->merge_polls = (uint32_t)lvspec_merge_polls(std::getenv("LVSPEC_MERGE_POLLS"));
     if (const char *e = std::getenv("LVSPEC_NO_PDL")) ctx->pdl = !(e[0] && e[0] != '0');
     // status word and counters, then the exchange buffer, in one allocation
-    const size_t counted = sizeof(uint32_t) * (1 + LVSPEC_MAX_BATCH + LVSPEC_MAX_BATCH * LVSPEC_MAX_GAMMA);
+    const size_t counted = sizeof(uint32_t) * (1 + LVSPEC_MAX_BATCH + LVSPEC_MAX_BATCH * LVSPEC_MAX_GAMMA + 1);
     const size_t small = (counted + 255) & ~size_t(255);
     ctx->exchange_bytes = kMergeWordBytes + (size_t)ctx->n_sm * LVSPEC_MAX_ROWS * (128 + 4) * sizeof(float);
     if ((e = cudaMalloc(reinterpret_cast<void **>(&ctx->status), small + ctx->exchange_bytes)) == cudaSuccess)
@@ -608,6 +651,7 @@ lvspec_status_t lvspec_create(lvspec_ctx_t **out, int device)
     }
     ctx->counters = ctx->status + 1;
     ctx->rel_counters = ctx->counters + LVSPEC_MAX_BATCH;
+    ctx->plan_ticket = ctx->rel_counters + LVSPEC_MAX_BATCH * LVSPEC_MAX_GAMMA;
     lvspec_status_t st = ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, size_t(8) << 20, true);
     if (st != LVSPEC_OK) {
         g_create_error = ctx->error;
@@ -962,6 +1006,182 @@ lvspec_status_t lvspec_verify_attention_fp8(lvspec_ctx_t *ctx, const lvspec_attn
     lvspec_attn_shape_t s = *shape;
     s.kernel = LVSPEC_KERNEL_TCGEN05;
     return run_attention(ctx, &s, seq, max_len, q, k_cache, v_cache, out, visual_mass, 0, nullptr, nullptr, &f8);
+}
+
+lvspec_status_t lvspec_plan_pages(lvspec_ctx_t *ctx, int32_t batch, int32_t page_size, int32_t pages_per_seq, int32_t n_pages,
+                                  int32_t max_new, const int32_t *kv_len, const int32_t *n_new, const int32_t *pages_held,
+                                  const int32_t *n_free, const int32_t *free_pages, int32_t *block_table, int32_t *new_kv_len,
+                                  int32_t *new_pages_held, int32_t *new_n_free, int32_t *token_start, int32_t *slot_map)
+{
+    if (!ctx) return LVSPEC_ERR_INVALID_ARG;
+    const void *all[] = {kv_len, n_new, pages_held, n_free, free_pages, block_table, new_kv_len, new_pages_held, new_n_free, token_start};
+    for (const void *a : all) {
+        if (!a) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "null argument");
+        if (!aligned4(a)) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "misaligned device pointer");
+    }
+    if (max_new < 0) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "max_new < 0");
+    if (max_new > 0 && !slot_map) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "null argument");
+    if (!aligned16(slot_map)) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "slot_map must be 16-byte aligned");
+    if (batch < 1 || batch > LVSPEC_MAX_REQUESTS) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "batch outside 1..LVSPEC_MAX_REQUESTS");
+    if (page_size < 1 || pages_per_seq < 1 || n_pages < 1 || (int64_t)n_pages * page_size > 2147483647ll ||
+        (int64_t)pages_per_seq * page_size > 2147483647ll)
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "page_size, pages_per_seq or n_pages out of range");
+    cudaError_t e = cudaSetDevice(ctx->device);
+    if (e != cudaSuccess) return cuda_fail(ctx, "cudaSetDevice", e);
+    PagePlanParams p;
+    std::memset(&p, 0, sizeof p);
+    p.kv_len = kv_len;
+    p.n_new = n_new;
+    p.pages_held = pages_held;
+    p.n_free = n_free;
+    p.free_pages = free_pages;
+    p.block_table = block_table;
+    p.new_kv_len = new_kv_len;
+    p.new_pages_held = new_pages_held;
+    p.new_n_free = new_n_free;
+    p.token_start = token_start;
+    p.slot_map = slot_map;
+    p.ticket = ctx->plan_ticket;
+    p.status = ctx->status;
+    p.batch = batch;
+    p.page_size = page_size;
+    p.pages_per_seq = pages_per_seq;
+    p.n_pages = n_pages;
+    p.max_new = max_new;
+    int launches = 0;
+    e = launch_page_plan(p, ctx->n_sm, ctx->pdl, ctx->stream, &launches);
+    ctx->launches += launches;
+    if (e != cudaSuccess) return cuda_fail(ctx, "page table kernel launch", e);
+    return LVSPEC_OK;
+}
+
+lvspec_status_t lvspec_append_paged_fp8(lvspec_ctx_t *ctx, int32_t n_tokens, int32_t n_kv_heads, int32_t head_dim,
+                                        const lvspec_paged_fp8_t *cache, const void *k, const void *v, int64_t k_token_stride,
+                                        int64_t v_token_stride, const int32_t *slot_map, void *k_pool, void *v_pool,
+                                        float *k_scale, float *v_scale)
+{
+    if (!ctx) return LVSPEC_ERR_INVALID_ARG;
+    if (n_tokens < 0) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "n_tokens < 0");
+    if (!cache || !k_pool || !v_pool || !k_scale || !v_scale || (n_tokens > 0 && (!k || !v || !slot_map)))
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "null argument");
+    if (n_kv_heads < 1 || n_kv_heads > 65535) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "n_kv_heads outside 1..65535");
+    if (head_dim != 64 && head_dim != 128) return fail(ctx, LVSPEC_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+    PagedFp8Layout lay;
+    lvspec_status_t st = check_paged_fp8(ctx, cache, n_kv_heads, head_dim, &lay);
+    if (st != LVSPEC_OK) return st;
+    for (const int64_t s : {k_token_stride, v_token_stride})
+        if (s < (int64_t)n_kv_heads * head_dim || (s & 7) || s >= (int64_t(1) << 32))
+            return fail(ctx, LVSPEC_ERR_INVALID_ARG, "token strides must be multiples of 8 elements, at least n_kv_heads * head_dim");
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned4(k_scale) || !aligned4(v_scale) ||
+        !aligned4(slot_map))
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "misaligned device pointer");
+    if (n_tokens == 0) return LVSPEC_OK;
+    cudaError_t e = cudaSetDevice(ctx->device);
+    if (e != cudaSuccess) return cuda_fail(ctx, "cudaSetDevice", e);
+    AppendFp8Params p;
+    std::memset(&p, 0, sizeof p);
+    p.k = static_cast<const uint16_t *>(k);
+    p.v = static_cast<const uint16_t *>(v);
+    p.k_stride = k_token_stride;
+    p.v_stride = v_token_stride;
+    p.slot_map = slot_map;
+    p.k_pool = static_cast<uint8_t *>(k_pool);
+    p.v_pool = static_cast<uint8_t *>(v_pool);
+    p.k_scale = k_scale;
+    p.v_scale = v_scale;
+    p.page_stride = lay.page;
+    p.head_stride = lay.head;
+    p.position_stride = lay.position;
+    p.n_tokens = n_tokens;
+    p.n_heads = n_kv_heads;
+    p.n_pages = cache->n_pages;
+    p.page_size = cache->page_size;
+    p.block_log2 = lay.block_log2;
+    int launches = 0;
+    e = launch_append_fp8(p, head_dim, ctx->pdl, ctx->stream, &launches);
+    ctx->launches += launches;
+    if (e != cudaSuccess) return cuda_fail(ctx, "cache append kernel launch", e);
+    return LVSPEC_OK;
+}
+
+size_t lvspec_attention_paged_fp8_workspace_bytes(const lvspec_ctx_t *ctx, const lvspec_attn_shape_t *shape)
+{
+    if (!ctx || !shape || shape->n_kv_heads < 1 || shape->gamma < 1 || shape->n_q_heads < shape->n_kv_heads || shape->head_dim < 1)
+        return 0;
+    const int64_t rows = (int64_t)shape->gamma * (shape->n_q_heads / shape->n_kv_heads);
+    return rows > LVSPEC_MAX_ROWS ? 0 : paged_fp8_scratch_bytes(ctx->n_sm, (int)rows, shape->head_dim);
+}
+
+lvspec_status_t lvspec_verify_attention_paged_fp8(lvspec_ctx_t *ctx, const lvspec_attn_shape_t *shape,
+                                                  const lvspec_paged_fp8_t *cache, int32_t n_branches, int32_t max_kv_len,
+                                                  const void *q, const void *k_pool, const void *v_pool, const float *k_scale,
+                                                  const float *v_scale, const int32_t *block_table, const int32_t *kv_len,
+                                                  const int32_t *visual_span, void *out, float *visual_mass)
+{
+    if (!ctx) return LVSPEC_ERR_INVALID_ARG;
+    if (!k_scale || !v_scale || !block_table)
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "null argument");
+    lvspec_status_t st = check_attention_shape(ctx, shape, q, k_pool, v_pool, kv_len, visual_span, out, visual_mass, true);
+    if (st != LVSPEC_OK) return st;
+    if (shape->kernel == LVSPEC_KERNEL_SIMT)
+        return fail(ctx, LVSPEC_ERR_UNSUPPORTED, "the paged fp8 cache needs the tcgen05 kernel");
+    if (shape->n_split != 0) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "n_split must be 0: the tiles are shared out on the device");
+    if (n_branches < 1 || shape->gamma % n_branches != 0)
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "gamma must be a positive multiple of n_branches");
+    PagedFp8Layout lay;
+    st = check_paged_fp8(ctx, cache, shape->n_kv_heads, shape->head_dim, &lay);
+    if (st != LVSPEC_OK) return st;
+    if (shape->kv_capacity % cache->page_size != 0)
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "kv_capacity must be a whole number of pages");
+    if (max_kv_len < 1 || max_kv_len > shape->kv_capacity)
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "max_kv_len outside 1..kv_capacity");
+    const int64_t tiles = (int64_t)shape->batch * shape->n_kv_heads * (((int64_t)max_kv_len + 127) / 128);
+    if (tiles > (int64_t(1) << 30)) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "batch * n_kv_heads * max_kv_len out of range");
+    if (!aligned4(k_scale) || !aligned4(v_scale) || !aligned4(block_table) || !aligned4(kv_len) || !aligned4(visual_span))
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "misaligned device pointer");
+    cudaError_t e = cudaSetDevice(ctx->device);
+    if (e != cudaSuccess) return cuda_fail(ctx, "cudaSetDevice", e);
+    PagedFp8Params p;
+    std::memset(&p, 0, sizeof p);
+    p.q = static_cast<const uint16_t *>(q);
+    p.out = static_cast<uint16_t *>(out);
+    p.mass = visual_mass;
+    p.status = ctx->status;
+    p.block_table = block_table;
+    p.kv_len = kv_len;
+    p.span = visual_span;
+    p.k_scale = k_scale;
+    p.v_scale = v_scale;
+    p.page_stride = lay.page;
+    p.head_stride = lay.head;
+    p.position_stride = lay.position;
+    p.B = shape->batch;
+    p.gamma = shape->gamma;
+    p.Hq = shape->n_q_heads;
+    p.Hkv = shape->n_kv_heads;
+    p.D = shape->head_dim;
+    p.G = p.Hq / p.Hkv;
+    p.M = p.gamma * p.G;
+    p.branch_len = p.gamma / n_branches;
+    p.page_size = cache->page_size;
+    p.pages_per_seq = shape->kv_capacity / cache->page_size;
+    p.n_pages = cache->n_pages;
+    p.block_log2 = lay.block_log2;
+    p.blocks_per_page = cache->page_size >> lay.block_log2;
+    p.max_len = max_kv_len;
+    p.n_cta = tiles < ctx->n_sm ? (int)tiles : ctx->n_sm;
+    p.pdl = ctx->pdl ? 1 : 0;
+    p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)p.D));
+    // (sized for every length, so that a step run once can be captured whatever its lengths)
+    st = ensure(ctx, &ctx->scratch, &ctx->scratch_bytes, paged_fp8_scratch_bytes(ctx->n_sm, p.M, p.D), false);
+    if (st != LVSPEC_OK) return st;
+    p.part_o = static_cast<float *>(ctx->scratch);
+    p.part_stat = p.part_o + (size_t)2 * p.n_cta * p.M * p.D;
+    int launches = 0;
+    e = launch_attn_paged_fp8(p, static_cast<const uint8_t *>(k_pool), static_cast<const uint8_t *>(v_pool), ctx->stream, &launches);
+    ctx->launches += launches;
+    if (e != cudaSuccess) return cuda_fail(ctx, "paged fp8 attention launch", e);
+    return LVSPEC_OK;
 }
 
 lvspec_status_t lvspec_verify_attention_host(lvspec_ctx_t *ctx, const lvspec_attn_shape_t *shape,

@@ -198,4 +198,48 @@ size_t relevance_scratch_bytes(int B, int K, int lv, int d);
 cudaError_t launch_wait_expiry(uint32_t *status, unsigned long long limit_ns, cudaStream_t stream,
                                int *launches);
 
+// Page tables of a step (page_plan.cu).
+struct PagePlanParams {
+    const int32_t *kv_len, *n_new, *pages_held, *n_free;
+    const int32_t *free_pages;          // [n_pages], the first *n_free of them free; the last is taken first
+    int32_t *block_table;               // [batch, pages_per_seq]
+    int32_t *new_kv_len, *new_pages_held, *new_n_free;
+    int32_t *token_start;               // [batch + 1]
+    int32_t *slot_map;                  // [max_new]
+    uint32_t *ticket, *status;
+    int32_t batch, page_size, pages_per_seq, n_pages, max_new;
+};
+cudaError_t launch_page_plan(const PagePlanParams &p, int n_sm, bool pdl, cudaStream_t stream, int *launches);
+
+// New rows into a paged E4M3 cache (cache_append_fp8.cu).
+struct AppendFp8Params {
+    const uint16_t *k, *v;              // [n_tokens, n_heads, D] bf16, rows k_stride / v_stride elements apart
+    long long k_stride, v_stride;
+    const int32_t *slot_map;            // [n_tokens]
+    uint8_t *k_pool, *v_pool;
+    float *k_scale, *v_scale;           // [n_pages, n_heads, page_size >> block_log2]
+    long long page_stride, head_stride, position_stride;     // of the pools, in bytes
+    int32_t n_tokens, n_heads, n_pages, page_size, block_log2;
+};
+cudaError_t launch_append_fp8(const AppendFp8Params &p, int head_dim, bool pdl, cudaStream_t stream, int *launches);
+
+// Attention on a paged E4M3 cache with a scale per block (verify_attn_paged_fp8.cu).
+struct PagedFp8Params {
+    const uint16_t *q;                  // [B, gamma, Hq, D] bf16
+    uint16_t *out;                      // the same
+    float *mass;                        // [B, gamma, Hq]
+    float *part_o, *part_stat;          // [2 n_cta, M, D] and [2 n_cta, M, 4]: m (log2 units), l, l_vis, unused
+    uint32_t *status;
+    const int32_t *block_table, *kv_len, *span;
+    const float *k_scale, *v_scale;     // [n_pages, Hkv, blocks_per_page]
+    long long page_stride, head_stride, position_stride;     // of the pools, in bytes
+    int32_t B, gamma, Hq, Hkv, D, G, M, branch_len;
+    int32_t page_size, pages_per_seq, n_pages, block_log2, blocks_per_page;
+    int32_t max_len, n_cta, pdl;
+    float scale_log2;                   // log2(e) / sqrt(D)
+};
+size_t paged_fp8_scratch_bytes(int n_cta, int M, int D);
+cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool, const uint8_t *v_pool, cudaStream_t stream,
+                                  int *launches);
+
 }  // namespace lvspec
