@@ -45,13 +45,14 @@ namespace {
 using namespace ptx;
 
 constexpr int kTilePos = 128;
-constexpr int kGroups = 2;                  // softmax groups of four warps, each on its share of the columns
 constexpr int kConvertWarp0 = 4, kSoftmaxWarp0 = 8;
+constexpr int kGroups = 4;                  // softmax groups of four warps
 constexpr int kSoftmaxThreads = 128 * kGroups;
 constexpr int kThreads = 32 * kSoftmaxWarp0 + kSoftmaxThreads;
 constexpr int kMergeWarps = 8;
-constexpr int kBufs = 2;                    // S^T, P^T and V^T buffers each
-constexpr float kFirst = 3.f;               // log2 of the probability of a segment's first position
+constexpr int kVBufs = 2;                   // V^T buffers in tensor memory
+constexpr int kMaxBufs = 4;                 // S^T buffers and P^T buffers, at most
+constexpr float kFirst = 3.f;               // log2 of the probability of a stream's first position
 constexpr float kGuard = 14.f;              // log2 units above the reference before it moves
 constexpr int kFlatGain = 3;                // tiles a straight cut has to save to be taken
 
@@ -70,56 +71,65 @@ __device__ __forceinline__ int padded(const Line &w, int tiles)
     return w.aligned ? (tiles + w.share - 1) / w.share * w.share : tiles;
 }
 
-// One warp.  True when a length lies outside 0..max_len (the sequence then counts as empty).
-__device__ __forceinline__ bool make_line(Line &w, const PagedFp8Params &p)
+// ceil(x / d) for x < 2^30 with m = 2^32 / d + 1 (0 for d = 1): the product is one too large at most
+__device__ __forceinline__ int ceil_div(int x, int d, uint32_t m)
 {
-    constexpr int kPer = LVSPEC_MAX_BATCH / 32;
+    const int y = x + d - 1;
+    if (m == 0u) return x;
+    const int q = (int)__umulhi((uint32_t)y, m);
+    return q * d > y ? q - 1 : q;
+}
+__device__ __forceinline__ uint32_t magic_of(uint32_t d) { return d > 1 ? 0xFFFFFFFFu / d + 1u : 0u; }
+
+// One warp.  True when a length lies outside 0..max_len (the sequence then counts as empty).
+__device__ __noinline__ bool make_line(Line &w, const int32_t *kv_len, int B, int Hkv, int max_len, int n_cta)
+{
     const int lane = threadIdx.x & 31;
-    int tiles[kPer], total = 0, longest = 0;
+    int total = 0;
     bool bad = false;
-#pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-        const int b = u * 32 + lane;
-        int len = b < p.B ? p.kv_len[b] : 0;
-        if (len < 0 || len > p.max_len) {
+#pragma unroll 1
+    for (int b = lane; b < B; b += 32) {
+        int len = kv_len[b];
+        if (len < 0 || len > max_len) {
             bad = true;
             len = 0;
         }
-        if (b < p.B) w.len[b] = len;
-        tiles[u] = tiles_of(len);
-        total += tiles[u];
-        longest = max(longest, tiles[u]);
+        w.len[b] = len;
+        total += tiles_of(len);
     }
-    total = __reduce_add_sync(0xffffffffu, total) * p.Hkv;
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    const int flat = max(1, (total + p.n_cta - 1) / p.n_cta);
+    total = __reduce_add_sync(0xffffffffu, total) * Hkv;
+    const int flat = max(1, (total + n_cta - 1) / n_cta);
     int share = flat, aligned = 0;
+    uint32_t magic = 0;
     // cutting within pairs is taken if it costs a few tiles at most: a second pair in a CTA costs as much
-    for (int t = flat; t <= flat + kFlatGain && !aligned; ++t) {
+#pragma unroll 1
+    for (int t = flat; t <= flat + kFlatGain; ++t) {
+        magic = magic_of(t);
         int ctas = 0;
-#pragma unroll
-        for (int u = 0; u < kPer; ++u)
-            if (u * 32 < p.B) ctas += (tiles[u] + t - 1) / t;
-        if (__reduce_add_sync(0xffffffffu, ctas) * p.Hkv <= p.n_cta) {
+#pragma unroll 1
+        for (int b = lane; b < B; b += 32) ctas += ceil_div(tiles_of(w.len[b]), t, magic);
+        if (__reduce_add_sync(0xffffffffu, ctas) * Hkv <= n_cta) {
             share = t;
             aligned = 1;
+            break;
         }
     }
     int before = 0;
-#pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-        if (u * 32 >= p.B) break;
-        int mine = (aligned ? (tiles[u] + share - 1) / share * share : tiles[u]) * p.Hkv, in = mine;
+#pragma unroll 1
+    for (int b0 = 0; b0 < B; b0 += 32) {
+        const int b = b0 + lane, tiles = b < B ? tiles_of(w.len[b]) : 0;
+        const int mine = (aligned ? ceil_div(tiles, share, magic) * share : tiles) * Hkv;
+        int in = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, in, o);
             if (lane >= o) in += y;
         }
-        if (u * 32 + lane < p.B) w.start[u * 32 + lane] = before + in - mine;
+        if (b < B) w.start[b] = before + in - mine;
         before += __shfl_sync(0xffffffffu, in, 31);
     }
     if (lane == 0) {
-        w.start[p.B] = before;
+        w.start[B] = before;
         w.share = share;
         w.aligned = aligned;
     }
@@ -132,62 +142,63 @@ struct Segment {
     bool first, last;                       // begins / ends its pair
 };
 struct Walk {
-    const Line &w;
-    const int n_seq;
     int at, end, b;
-    __device__ __forceinline__ Walk(const Line &w_, int n_seq_, int cta) : w(w_), n_seq(n_seq_), b(0)
+    __device__ __forceinline__ Walk(const Line &w, int n_seq, int cta) : b(0)
     {
         at = cta * w.share;
         end = min(at + w.share, w.start[n_seq]);
-        int hi = n_seq;
-        while (hi - b > 1) {
-            const int mid = (b + hi) >> 1;
-            if (w.start[mid] <= at) b = mid;
-            else hi = mid;
-        }
-    }
-    __device__ __forceinline__ bool next(Segment &s)
-    {
-        if (at >= end) return false;
-        while (at >= w.start[b + 1]) ++b;
-        s.b = b;
-        s.len = w.len[b];
-        s.tiles = tiles_of(s.len);
-        const int each = padded(w, s.tiles), off = at - w.start[b];
-        s.head = off / each;
-        s.t0 = off - s.head * each;
-        const int stop = min(end, w.start[b] + (s.head + 1) * each);
-        s.T = min(s.tiles - s.t0, stop - at);
-        s.first = s.t0 == 0;
-        s.last = s.t0 + s.T == s.tiles;
-        at = stop;
-        return true;
     }
 };
+// (out of line: six roles step through their segments, and what counts in this kernel is that its loops stay in the
+// instruction caches)
+__device__ __noinline__ bool next_segment(const Line &w, Walk &walk, Segment &s)
+{
+    if (walk.at >= walk.end) return false;
+    int b = walk.b;
+    while (walk.at >= w.start[b + 1]) ++b;
+    s.b = walk.b = b;
+    s.len = w.len[b];
+    s.tiles = tiles_of(s.len);
+    const int each = padded(w, s.tiles), off = walk.at - w.start[b];
+    s.head = off / each;
+    s.t0 = off - s.head * each;
+    const int stop = min(walk.end, w.start[b] + (s.head + 1) * each);
+    s.T = min(s.tiles - s.t0, stop - walk.at);
+    s.first = s.t0 == 0;
+    s.last = s.t0 + s.T == s.tiles;
+    walk.at = stop;
+    return true;
+}
 // Partial results of a CTA: of the pair it goes on with, and of the pair it begins and does not end.
 __device__ __forceinline__ int part_slot(int cta, bool first) { return 2 * cta + (first ? 1 : 0); }
 
 // ---- shared memory --------------------------------------------------------------------
 struct Smem {
-    uint32_t k, v, q, p, m, tmx, sums, bars, misc, line, total;
+    uint32_t k, v, q, p, nm, tmx, fac, sums, rows, scale, bars, misc, line, total;
     int ks, vs;                             // K and V slots
+    int s_log2, p_log2;                     // S^T and P^T buffers
 };
-constexpr int kBarsFixed = 6 * kBufs + 3;
-Smem smem_map(int D, int NP, int ks, int vs)
+constexpr int kBarsFixed = 5 * kMaxBufs + 2 * kVBufs + 4;
+Smem smem_map(int D, int NP, int streams, int ks, int vs, int s_log2, int p_log2)
 {
     Smem s;
     uint32_t o = 0;
     s.ks = ks;
     s.vs = vs;
+    s.s_log2 = s_log2;
+    s.p_log2 = p_log2;
     s.k = o;    o += ks * kTilePos * D;
     s.v = o;    o += vs * kTilePos * D;
     s.q = o;    o += 2 * NP * D;
-    s.p = o;    o += kBufs * NP * 256;
-    s.m = o;    o += NP * 4;
-    s.tmx = o;  o += 4 * NP * 4;
-    s.sums = o; o += 2 * 4 * NP * 4;
+    s.p = o;    o += (NP * 256) << p_log2;
+    s.nm = o;   o += streams * NP * 4;            // [stream][NP]: minus the reference exponents
+    s.tmx = o;  o += streams * 4 * NP * 4;  // [stream][warp of the group][NP]: a tile's maxima
+    s.fac = o;  o += streams * NP * 4;      // [stream][NP]: what a move multiplies by; the streams' weights at the end
+    s.sums = o; o += streams * 2 * 4 * NP * 4;   // [stream][all, inside the span][warp of the group][NP]
+    s.rows = o; o += NP * 4;
+    s.scale = o; o += kMaxBufs * 16 * 4;    // [S^T buffer][K, V][block of the tile]
     s.bars = o; o += 8 * (2 * ks + 2 * vs + kBarsFixed);
-    s.misc = o; o += 64;                    // TMEM address, abort flag, per-warp maxima
+    s.misc = o; o += 128;                   // TMEM address, abort flag, words of the softmax warps and groups
     s.line = o; o += (sizeof(Line) + 15) & ~15u;
     s.total = o;
     return s;
@@ -211,6 +222,29 @@ struct Ring {
         }
     }
 };
+// tile n's place in a ring of 2^log2 buffers, and the parity of its round
+__device__ __forceinline__ int place(int n, int log2) { return n & ((1 << log2) - 1); }
+__device__ __forceinline__ uint32_t round_of(int n, int log2) { return (uint32_t)(n >> log2) & 1u; }
+
+// Bounded wait (about two seconds, then the CTA's abort flag is raised): as mbar_wait, in fewer instructions.
+__device__ __forceinline__ uint32_t timer_lo()
+{
+    uint32_t t;
+    asm volatile("mov.u32 %0, %globaltimer_lo;" : "=r"(t));
+    return t;
+}
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint32_t t0 = timer_lo();
+    while (!mbar_try_wait(bar, parity)) {
+        if (*abort_flag) return false;
+        if (timer_lo() - t0 > 2000000000u) *abort_flag = 1;
+    }
+    return true;
+}
+// 2^k, k within -126 .. 127
+__device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }
 
 __device__ __forceinline__ bool wait_unconditional(uint32_t bar, uint32_t parity)
 {
@@ -323,20 +357,98 @@ __device__ __forceinline__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_
 }
 constexpr uint32_t kSwizzle64B = 4;
 
-// Sum of each of eight values over the warp: lane t with t % 4 == 0 gets that of value t / 4 (bits 4, 3, 2
-// of the lane, highest first).  Nine shuffles where eight plain sums take forty.
-__device__ __forceinline__ float sum8(const float (&v)[8], int lane)
+// Sums of kN (8 or 4) values over the warp's lanes (kN = 4: over those that agree in bit 4, which tells whose four
+// values they are).  Lanes with lane % 4 == 0 get the sum of value number (bits 4, 3, 2 of the lane, or bits 3, 2), the
+// highest bit first: nine (five) shuffles where plain sums take forty (sixteen).
+template <int kN>
+__device__ __forceinline__ float warp_sums(const float *v, int lane)
 {
     float a[4], b[2], c;
     const bool h16 = lane & 16, h8 = lane & 8, h4 = lane & 4;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = (h16 ? v[k + 4] : v[k]) + __shfl_xor_sync(0xffffffffu, h16 ? v[k] : v[k + 4], 16);
+    for (int k = 0; k < 4; ++k) {
+        if (kN == 8) a[k] = (h16 ? v[k + 4] : v[k]) + __shfl_xor_sync(0xffffffffu, h16 ? v[k] : v[k + 4], 16);
+        else a[k] = v[k];
+    }
 #pragma unroll
     for (int k = 0; k < 2; ++k) b[k] = (h8 ? a[k + 2] : a[k]) + __shfl_xor_sync(0xffffffffu, h8 ? a[k] : a[k + 2], 8);
     c = (h4 ? b[1] : b[0]) + __shfl_xor_sync(0xffffffffu, h4 ? b[0] : b[1], 4);
     c += __shfl_xor_sync(0xffffffffu, c, 2);
     c += __shfl_xor_sync(0xffffffffu, c, 1);
     return c;
+}
+
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi) { return pack_f32x2(__float_as_uint(lo), __float_as_uint(hi)); }
+// Scaled scores x of eight columns: score * ck + (minus the reference)
+template <bool kMask>
+__device__ __forceinline__ void scores8(const uint32_t *raw, const float *nm, float ck, Seen seen, int col, float (&x)[8])
+{
+    const uint64_t c2 = pair(ck, ck);
+    const ulonglong2 na = *reinterpret_cast<const ulonglong2 *>(nm), nb = *reinterpret_cast<const ulonglong2 *>(nm + 4);
+    const uint64_t n2[4] = {na.x, na.y, nb.x, nb.y};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) unpack_f32x2(fma_f32x2(pack_f32x2(raw[2 * k], raw[2 * k + 1]), c2, n2[k]), x[2 * k], x[2 * k + 1]);
+    if (kMask)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = seen(col + k) ? x[k] : -INFINITY;
+}
+
+// Sums a thread keeps: of all eight columns of a chunk, or (kHalf, many rows) of four, the other four having gone to the lane
+// 16 away, whose own four come here.
+__device__ __forceinline__ void own4(const float (&e)[8], int lane, float (&t)[4])
+{
+    const bool hi = lane & 16;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) t[k] = (hi ? e[k + 4] : e[k]) + __shfl_xor_sync(0xffffffffu, hi ? e[k] : e[k + 4], 16);
+}
+
+// One tile, one position, up to kC chunks of eight columns: probabilities into P^T and (times sign) the sums; returns the largest
+// scaled score.
+template <int kC, bool kHalf, bool kMask>
+__device__ __forceinline__ float softmax_pass(uint32_t s_addr, const float *nm, float ck, float vsr, Seen seen, int col0,
+                                              uint8_t *prow, int lane, float sign, float (&l)[kC * (kHalf ? 4 : 8)])
+{
+    float top = -INFINITY;
+    uint32_t raw[2][8];
+    tmem_ld_x8(s_addr, raw[0]);
+    const uint64_t v2 = pair(vsr, vsr), s2 = pair(sign, sign);
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+        tmem_wait_ld();
+        if (c + 1 < kC) tmem_ld_x8(s_addr + (c + 1) * 8, raw[(c + 1) & 1]);
+        float x[8];
+        scores8<kMask>(raw[c & 1], nm + c * 8, ck, seen, col0 + c * 8, x);
+        top = fmaxf(top, fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = ex2(x[k]);
+        if constexpr (kHalf) {
+            float t[4];
+            own4(x, lane, t);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) l[c * 4 + k] = fmaf(sign, t[k], l[c * 4 + k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint64_t t = fma_f32x2(s2, pair(x[2 * k], x[2 * k + 1]), pair(l[c * 8 + 2 * k], l[c * 8 + 2 * k + 1]));
+                unpack_f32x2(t, l[c * 8 + 2 * k], l[c * 8 + 2 * k + 1]);
+            }
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float a, b;
+            unpack_f32x2(mul_f32x2(pair(x[2 * k], x[2 * k + 1]), v2), a, b);
+            w[k] = pack_f16x2(a, b);
+        }
+        *reinterpret_cast<uint4 *>(prow + c * 2048) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return top;
 }
 
 __device__ __forceinline__ int div_by(int x, int d, uint32_t m)
@@ -346,8 +458,10 @@ __device__ __forceinline__ int div_by(int x, int d, uint32_t m)
     return q * d > x ? q - 1 : q;
 }
 
-// kC: chunks of eight columns a softmax group has at most
-template <int kC>
+// The softmax groups take the tiles in turn, kStreams of them, each with its own references, sums and accumulators of O (a
+// stream), put together when the segment ends; the groups of a stream (4 / kStreams) share out the columns, at most kC chunks of
+// eight to a group.
+template <int kStreams, int kC, bool kHalf>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v)
 {
@@ -356,12 +470,12 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
     const Smem &sm = P.sm;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int D = p.D, NP = P.NP, M = p.M, G = p.G, gamma = p.gamma;
-    const int n8 = (M + 7) >> 3;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *gbase = smem_raw + (base - smem_u32(smem_raw));
-    float *m_s = reinterpret_cast<float *>(gbase + sm.m);
-    float *tmx_s = reinterpret_cast<float *>(gbase + sm.tmx);
-    float *sums_s = reinterpret_cast<float *>(gbase + sm.sums);      // [outside, inside the span][warp of the group][NP]
+    float *nm_s = reinterpret_cast<float *>(gbase + sm.nm), *fac_s = reinterpret_cast<float *>(gbase + sm.fac);
+    float *sums_s = reinterpret_cast<float *>(gbase + sm.sums);
+    float *scale_s = reinterpret_cast<float *>(gbase + sm.scale);
+    int *row_s = reinterpret_cast<int *>(gbase + sm.rows);           // output row of each column
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(gbase + sm.misc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + sm.misc + 4);
     volatile uint32_t *wmax_s = reinterpret_cast<volatile uint32_t *>(gbase + sm.misc + 16);
@@ -374,12 +488,16 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
     auto v_full = [&](int s) { return bar0 + 8 * (2 * sm.ks + s); };
     auto v_empty = [&](int s) { return bar0 + 8 * (2 * sm.ks + sm.vs + s); };
     const uint32_t bar1 = bar0 + 8 * (2 * sm.ks + 2 * sm.vs);
-    auto s_full = [&](int s) { return bar1 + 8 * s; };
-    auto s_free = [&](int s) { return bar1 + 8 * (kBufs + s); };
-    auto p_full = [&](int s) { return bar1 + 8 * (2 * kBufs + s); };
-    auto vt_full = [&](int s) { return bar1 + 8 * (3 * kBufs + s); };
-    auto pv_done = [&](int s) { return bar1 + 8 * (4 * kBufs + s); };      // frees the P^T and the V^T buffer
-    const uint32_t q_full = bar1 + 8 * 5 * kBufs, o_free = q_full + 8, drain_qk = q_full + 16, drain_pv = q_full + 24;
+    auto s_full = [&](int n) { return bar1 + 8 * place(n, sm.s_log2); };
+    auto s_free = [&](int n) { return bar1 + 8 * (kMaxBufs + place(n, sm.s_log2)); };
+    auto p_full = [&](int n) { return bar1 + 8 * (2 * kMaxBufs + place(n, sm.p_log2)); };
+    auto pv_done = [&](int n) { return bar1 + 8 * (3 * kMaxBufs + place(n, sm.p_log2)); };
+    auto sc_full = [&](int n) { return bar1 + 8 * (4 * kMaxBufs + place(n, sm.s_log2)); };     // the tile's scales are there
+    const uint32_t bar2 = bar1 + 8 * 5 * kMaxBufs;
+    auto vt_full = [&](int s) { return bar2 + 8 * s; };
+    auto vt_free = [&](int s) { return bar2 + 8 * (kVBufs + s); };
+    const uint32_t q_full = bar2 + 8 * 2 * kVBufs, o_free = q_full + 8, drain_qk = q_full + 16, drain_pv = q_full + 24;
+    constexpr int kShare = kGroups / kStreams;              // groups that work on a tile
 
     if (warp == 3 && lane < 2) prefetch_tensormap(lane ? &tmap_v : &tmap_k);
     if (warp == 0) {
@@ -387,28 +505,27 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         for (int i = lane; i < n_bars; i += 32) {
             const int j = i - 2 * (sm.ks + sm.vs);
             uint32_t count = 1;
-            if (j < 0) count = i >= 2 * sm.ks + sm.vs ? D / 32 : 1;                 // v_empty: the converting warps
-            else if (j >= kBufs && j < 3 * kBufs) count = 4 * kGroups;              // s_free, p_full
-            else if (j >= 3 * kBufs && j < 4 * kBufs) count = D / 32;               // vt_full
-            else if (j == 5 * kBufs || j == 5 * kBufs + 1) count = 4 * kGroups;     // q_full, o_free
+            if (j < 0) count = i >= 2 * sm.ks + sm.vs ? D / 32 : 1;                             // v_empty: the converting warps
+            else if (j >= kMaxBufs && j < 3 * kMaxBufs) count = 4 * kShare;                     // s_free, p_full
+            else if (j >= 5 * kMaxBufs && j < 5 * kMaxBufs + kVBufs) count = D / 32;            // vt_full
+            else if (j == 5 * kMaxBufs + 2 * kVBufs || j == 5 * kMaxBufs + 2 * kVBufs + 1) count = 4 * kGroups;     // q_full, o_free
             mbar_init(bar0 + 8 * i, count);
         }
         if (lane == 0) *abort_flag = 0;
         fence_proxy_async_smem();
         grid_dependency_wait();
         grid_launch_dependents();
-        const bool bad = make_line(line, p);
+        const bool bad = make_line(line, p.kv_len, p.B, p.Hkv, p.max_len, p.n_cta);
         if (bad && blockIdx.x == 0 && lane == 0) atomicOr(p.status, LVSPEC_DEV_BAD_LENGTH);
     } else {
         if (warp == 1) {
             tmem_alloc(base + sm.misc, (uint32_t)P.tmem_cols);
             tmem_relinquish();
         }
-        // columns beyond the last chunk stay zero (at most one chunk per P^T buffer)
-        if (warp >= kSoftmaxWarp0 && n8 * 8 < NP) {
-            const int i = tid - 32 * kSoftmaxWarp0;      // 0..255: buffer, position
-            static_assert(kBufs * 128 == kSoftmaxThreads, "one 16-byte chunk a thread");
-            *reinterpret_cast<uint4 *>(gbase + sm.p + (i >> 7) * (NP * 256) + n8 * 2048 + (i & 127) * 16) = make_uint4(0, 0, 0, 0);
+        // one chunk of columns, and the product takes two: the second stays zero
+        if (kC == 1 && warp >= kSoftmaxWarp0) {
+            for (int i = tid - 32 * kSoftmaxWarp0; i < 128 << sm.p_log2; i += kSoftmaxThreads)
+                *reinterpret_cast<uint4 *>(gbase + sm.p + (i >> 7) * (NP * 256) + 2048 + (i & 127) * 16) = make_uint4(0, 0, 0, 0);
             fence_proxy_async_smem();
         }
         grid_dependency_wait();
@@ -417,7 +534,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    const uint32_t tm_v = tmem, tm_s = tmem + kBufs * 64, tm_o = tm_s + kBufs * NP;
+    const uint32_t tm_v = tmem, tm_o = tmem + kVBufs * 64, tm_s = tm_o + kStreams * NP;
 
     Walk walk(line, p.B, blockIdx.x);
     Segment seg;
@@ -430,7 +547,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         const uint32_t box_bytes = slot_bytes / boxes;
         int n = 0;                                     // tiles asked for
         bool ok = true;
-        while (ok && walk.next(seg)) {
+        while (ok && next_segment(line, walk, seg)) {
             const int32_t *row = p.block_table + (size_t)seg.b * p.pages_per_seq;
             const int n_live = (seg.len + p.page_size - 1) / p.page_size;
             // 32 entries of the block table at a time, the next 32 on their way
@@ -448,13 +565,13 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                     nxt = entries(have + 32);
                 }
                 const int page = __shfl_sync(0xffffffffu, cur, (at.page + (lane < boxes ? lane : 0)) & 31);
-                if (n >= sm.ks) ok = mbar_wait(k_empty(kr.idx), kr.parity ^ 1u, abort_flag);
+                if (n >= sm.ks) ok = wait(k_empty(kr.idx), kr.parity ^ 1u, abort_flag);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 const uint32_t kd = base + sm.k + kr.idx * slot_bytes, vd = base + sm.v + vr.idx * slot_bytes;
                 if (lane == 0) mbar_arrive_expect_tx(k_full(kr.idx), slot_bytes);
                 __syncwarp();
                 if (lane < boxes) tma_load_4d_hint(kd + lane * box_bytes, &tmap_k, k_full(kr.idx), 0, at.off, seg.head, page, policy);
-                if (n >= sm.vs) ok = mbar_wait(v_empty(vr.idx), vr.parity ^ 1u, abort_flag);
+                if (n >= sm.vs) ok = wait(v_empty(vr.idx), vr.parity ^ 1u, abort_flag);
                 if (!__all_sync(0xffffffffu, ok)) {
                     ok = false;
                     kr.next(sm.ks);
@@ -478,31 +595,34 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         const uint32_t idesc = make_idesc_e4m3(128, NP, 0, 0);
         const uint32_t swz = D == 128 ? kSwizzle128B : kSwizzle64B;
         const uint64_t kd0 = make_smem_desc(base + sm.k, 16, 8 * D, swz), qd0 = make_smem_desc(base + sm.q, 16, 8 * D, swz);
-        const int steps = D / 32;
-        Ring kr, sr, qr;
+        const uint32_t rest = (uint32_t)(NP * D) >> 4;
+        Ring kr, qr;
         int n = 0;
         bool ok = true;
-        while (ok && walk.next(seg)) {
-            ok = mbar_wait(q_full, qr.parity, abort_flag);
+        while (ok && next_segment(line, walk, seg)) {
+            ok = wait(q_full, qr.parity, abort_flag);
             qr.next(1);
             for (int j = 0; ok && j < seg.T; ++j, ++n) {
-                ok = mbar_wait(k_full(kr.idx), kr.parity, abort_flag);
-                if (n >= kBufs) ok = mbar_wait(s_free(sr.idx), sr.parity ^ 1u, abort_flag) && ok;
+                ok = wait(k_full(kr.idx), kr.parity, abort_flag);
+                if (n >> sm.s_log2) ok = wait(s_free(n), round_of(n, sm.s_log2) ^ 1u, abort_flag) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
                     const uint64_t kd = kd0 + (uint64_t)(kr.idx * (slot_bytes >> 4));
+                    const uint32_t d = tm_s + place(n, sm.s_log2) * NP;
                     // q's leading bits, then the rest
-                    for (int t = 0; t < 2; ++t)
-                        for (int c = 0; c < steps; ++c)
-                            mma_f8_ss(tm_s + sr.idx * NP, kd + 2 * c, qd0 + (uint64_t)(t * (NP * D >> 4) + 2 * c), idesc, t + c > 0);
-                    mma_commit(s_full(sr.idx));
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (c < 2 || D == 128) mma_f8_ss(d, kd + 2 * c, qd0 + 2 * c, idesc, c > 0);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (c < 2 || D == 128) mma_f8_ss(d, kd + 2 * c, qd0 + (rest + 2 * c), idesc, 1);
+                    mma_commit(s_full(n));
                     mma_commit(k_empty(kr.idx));
                 }
                 __syncwarp();
                 kr.next(sm.ks);
-                sr.next(kBufs);
             }
         }
         if (elect_one()) {
@@ -514,29 +634,31 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         // ------------------------------------------------------------ P.V issuer
         const uint32_t idesc = make_idesc_f16(128, NP, 1);
         const uint64_t pd0 = make_smem_desc(base + sm.p, 128, 2048, kSwizzleNone);
-        Ring br, orr;
-        int n_seg = 0;
+        Ring vr, orr;
+        int n = 0;
         bool ok = true;
-        while (ok && walk.next(seg)) {
-            if (n_seg++ > 0) {
-                ok = mbar_wait(o_free, orr.parity, abort_flag);     // the accumulators of the segment before have been read
+        while (ok && next_segment(line, walk, seg)) {
+            if (n > 0) {
+                ok = wait(o_free, orr.parity, abort_flag);     // the accumulators of the segment before have been read
                 orr.next(1);
             }
-            for (int j = 0; ok && j < seg.T; ++j) {
-                ok = mbar_wait(vt_full(br.idx), br.parity, abort_flag) && ok;
-                ok = mbar_wait(p_full(br.idx), br.parity, abort_flag) && ok;
+            for (int j = 0; ok && j < seg.T; ++j, ++n) {
+                ok = wait(vt_full(vr.idx), vr.parity, abort_flag) && ok;
+                ok = wait(p_full(n), round_of(n, sm.p_log2), abort_flag) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t pd = pd0 + (uint64_t)(br.idx * (NP * 256 >> 4));
+                    const uint64_t pd = pd0 + (uint64_t)(place(n, sm.p_log2) * (NP * 256 >> 4));
+                    const uint32_t d = tm_o + (j & (kStreams - 1)) * NP;
 #pragma unroll
                     for (int c = 0; c < 8; ++c)
-                        mma_f16_ts(tm_o, tm_v + br.idx * 64 + c * 8, pd + (uint64_t)(c * 16), idesc, j + c > 0);
-                    mma_commit(pv_done(br.idx));
+                        mma_f16_ts(d, tm_v + vr.idx * 64 + c * 8, pd + (uint64_t)(c * 16), idesc, j >= kStreams || c > 0);
+                    mma_commit(vt_free(vr.idx));
+                    mma_commit(pv_done(n));
                 }
                 __syncwarp();
-                br.next(kBufs);
+                vr.next(kVBufs);
             }
         }
         if (elect_one()) {
@@ -550,36 +672,39 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         Ring vr, br;
         int n = 0;
         bool ok = 32 * wq < D;
-        while (ok && walk.next(seg)) {
+        while (ok && next_segment(line, walk, seg)) {
             for (int j = 0; ok && j < seg.T; ++j, ++n) {
-                ok = mbar_wait(v_full(vr.idx), vr.parity, abort_flag);
-                if (n >= kBufs) ok = mbar_wait(pv_done(br.idx), br.parity ^ 1u, abort_flag) && ok;
+                ok = wait(v_full(vr.idx), vr.parity, abort_flag);
+                if (n >= kVBufs) ok = wait(vt_free(br.idx), br.parity ^ 1u, abort_flag) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 const int live = seg.len - (seg.t0 + j) * kTilePos;      // positions of this tile below the length
                 const uint32_t tile = base + sm.v + vr.idx * slot_bytes;
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
-                    uint32_t w[32];
+                    uint32_t r[4][4], w[32];
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
                         const int pos = u * 32 + lane, chunk = wq * 2 + h;
                         const int phase = D == 128 ? pos & 7 : (pos >> 1) & 3;
-                        uint32_t r[4];
-                        ldmatrix_b8_x2(tile + pos * D + ((chunk ^ phase) << 4), r);
-                        if (live < kTilePos) {
-                            // what lies behind the sequence is not the cache's: it may be anything, NaN among it
+                        ldmatrix_b8_x2(tile + pos * D + ((chunk ^ phase) << 4), r[u]);
+                    }
+                    if (__builtin_expect(live < kTilePos, 0)) {
+                        // what lies behind the sequence is not the cache's: it may be anything, NaN among it
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
                                 const int left = live - (u * 32 + (k >> 1) * 16 + (lane & 3) * 4);
-                                if (left < 4) r[k] &= left <= 0 ? 0u : 0xFFFFFFFFu >> (8 * (4 - left));
+                                if (left < 4) r[u][k] &= left <= 0 ? 0u : 0xFFFFFFFFu >> (8 * (4 - left));
                             }
-                        }
-                        // matrix m of this pair holds registers 2 m (row) and 2 m + 1 (row + 8)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) decode4(r[k], w[u * 8 + k * 2], w[u * 8 + k * 2 + 1]);
                     }
+                    // matrix m of a pair holds registers 2 m (row) and 2 m + 1 (row + 8)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) decode4(r[u][k], w[u * 8 + k * 2], w[u * 8 + k * 2 + 1]);
                     if (h == 1) {
                         __syncwarp();
                         if (lane == 0) mbar_arrive(v_empty(vr.idx));
@@ -591,88 +716,103 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 __syncwarp();
                 if (lane == 0) mbar_arrive(vt_full(br.idx));
                 vr.next(sm.vs);
-                br.next(kBufs);
+                br.next(kVBufs);
+            }
+        }
+    } else if (warp == 3) {
+        // ------------------------------------------------- the blocks' scales, from global to shared memory
+        // lanes 0..7 the K scales of a tile's blocks, 16..23 the V scales
+        const int blk = lane & 15, in_tile = blk << p.block_log2;
+        const float *from = lane < 16 ? p.k_scale : p.v_scale;
+        int n = 0;
+        bool ok = true;
+        while (ok && next_segment(line, walk, seg)) {
+            const int32_t *row = p.block_table + (size_t)seg.b * p.pages_per_seq;
+            PageWalk at(p, seg.t0, min(in_tile, kTilePos - 1));
+            int pos = seg.t0 * kTilePos + in_tile;
+            const int stop = min(seg.len, (seg.t0 + seg.T) * kTilePos);
+            // entry of the block table three tiles ahead, the scale itself two
+            int e = -1, off = 0;
+            float v0 = 0.f, v1 = 0.f;
+#pragma unroll 1
+            for (int j = -3; ok && j < seg.T; ++j) {
+                if (j >= 0) {
+                    if (n >> sm.s_log2) ok = wait(s_free(n), round_of(n, sm.s_log2) ^ 1u, abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (blk < 8) scale_s[place(n, sm.s_log2) * 16 + (lane >> 4) * 8 + blk] = v0;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sc_full(n));
+                    ++n;
+                }
+                v0 = v1;
+                v1 = e < 0 ? 0.f : from[((size_t)e * p.Hkv + seg.head) * p.blocks_per_page + (off >> p.block_log2)];
+                e = in_tile < kTilePos && pos < stop ? row[at.page] : -1;
+                if ((unsigned)e >= (unsigned)p.n_pages) e = -1;
+                off = at.off;
+                at.next_tile(p);
+                pos += kTilePos;
             }
         }
     } else if (warp >= kSoftmaxWarp0) {
         // ------------------------------------------------------------ softmax
         const int grp = (warp - kSoftmaxWarp0) >> 2, bar_id = 1 + grp;
+        constexpr int kAll = 1 + kGroups;                       // barrier of all softmax threads
+        const int stream = grp / kShare, part = grp % kShare;
         const int wq = warp & 3, row = wq * 32 + lane;          // TMEM lane: position of the tile, channel of the output
-        const int stid = tid - 32 * kSoftmaxWarp0;
+        const int stid = tid - 32 * kSoftmaxWarp0, gtid = stid & 127;
         const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
-        const int c_lo = grp == 0 ? 0 : (n8 + 1) / 2, n_c = grp == 0 ? (n8 + 1) / 2 : n8 / 2, col0 = c_lo * 8;
-        float *my_sums = sums_s + wq * NP + col0;
-        Ring sr, br, done;
-        int n = 0;
+        // this group's chunks of columns
+        const int c_lo = part * kC, col0 = c_lo * 8;
+        constexpr int kEach = kHalf ? 4 : 8;                    // sums a thread keeps of a chunk
+        float *nm = nm_s + stream * NP + col0, *fac = fac_s + stream * NP + col0;
+        float *tmx = reinterpret_cast<float *>(gbase + sm.tmx) + stream * 4 * NP + col0;
+        float *my_sums = sums_s + (stream * 8 + wq) * NP + col0;            // + 4 NP: inside the span
+        int n0 = 0;                                             // tiles of the segments before
         // No wait ends a loop here: a warp that left would leave its group at a barrier.  After a wait has run out all
         // others end at once, and what is computed then is void.
-        while (walk.next(seg)) {
+        while (next_segment(line, walk, seg)) {
             const int L = seg.len;
             const int vis0 = p.span[2 * seg.b], vis1 = p.span[2 * seg.b + 1];
-            const int32_t *table = p.block_table + (size_t)seg.b * p.pages_per_seq;
-            // ---- scales, asked for ahead: the table's entry two tiles, the scale one tile
-            PageWalk at(p, seg.t0, row);
-            int pos_e = seg.t0 * kTilePos + row;
-            auto entry = [&]() {
-                const int e = pos_e < L ? table[at.page] : -1;
-                pos_e += kTilePos;
-                return (unsigned)e < (unsigned)p.n_pages ? e : -1;
-            };
-            auto scales = [&](int e, int off, float &k, float &v) {
-                k = v = 0.f;
-                if (e < 0) return;
-                const size_t i = ((size_t)e * p.Hkv + seg.head) * p.blocks_per_page + (off >> p.block_log2);
-                k = p.k_scale[i];
-                v = p.v_scale[i];
-            };
-            int e_next = entry(), off_next = at.off;
-            float ks, vs, ks_next, vs_next;
-            scales(e_next, off_next, ks_next, vs_next);
-            at.next_tile(p);
-            e_next = entry();
-            off_next = at.off;
 
             // ---- q as two E4M3 operand tiles
             float scale;
             {
-                const int per_row = D / 8, n_chunks = NP * per_row;
-                constexpr int kMine = (kC * 16 * 16 + kSoftmaxThreads - 1) / kSoftmaxThreads;   // 16-byte chunks of a thread
-                uint4 qv[kMine];
+                const int per_log2 = D == 128 ? 4 : 3, n_chunks = NP << per_log2;          // chunks of eight channels
+                const uint16_t *q = p.q + ((size_t)seg.b * gamma * p.Hq + seg.head * G) * D;
+                auto load = [&](int ch) {
+                    const int r = ch >> per_log2, c = ch & ((1 << per_log2) - 1);
+                    if (ch >= n_chunks || r >= M) return make_uint4(0, 0, 0, 0);
+                    const int g = div_by(r, G, P.group_magic), hg = r - g * G;
+                    return *reinterpret_cast<const uint4 *>(q + ((size_t)g * p.Hq + hg) * D + c * 8);
+                };
+                // a thread's first two chunks (all of them up to 64 rows) stay in registers
+                uint4 qv[2] = {load(stid), load(stid + kSoftmaxThreads)};
                 uint32_t amax = 0;
-#pragma unroll
-                for (int u = 0; u < kMine; ++u) {
-                    const int ch = stid + u * kSoftmaxThreads;
-                    qv[u] = make_uint4(0, 0, 0, 0);
-                    if (ch < n_chunks) {
-                        const int r = D == 128 ? ch >> 4 : ch >> 3, c = ch & (per_row - 1);
-                        if (r < M) {
-                            const int g = div_by(r, G, P.group_magic), hg = r - g * G;
-                            qv[u] = *reinterpret_cast<const uint4 *>(
-                                p.q + (((size_t)seg.b * gamma + g) * p.Hq + seg.head * G + hg) * D + c * 8);
-                        }
-                        const uint32_t w[4] = {qv[u].x, qv[u].y, qv[u].z, qv[u].w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) amax = max(amax, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
-                    }
-                }
+                auto largest = [&](uint4 x) {
+                    // (of either half, as integers: without their signs bf16 values order as their bits do)
+                    const uint32_t a = __vmaxu2(__vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
+                    amax = max(amax, max(a & 0xFFFFu, a >> 16));
+                };
+                largest(qv[0]);
+                largest(qv[1]);
+#pragma unroll 1
+                for (int ch = stid + 2 * kSoftmaxThreads; ch < n_chunks; ch += kSoftmaxThreads) largest(load(ch));
                 amax = __reduce_max_sync(0xffffffffu, amax);
-                // (a segment's first barrier: nobody still reads the last one's maxima, its epilogue lies between)
                 if (lane == 0) wmax_s[warp - kSoftmaxWarp0] = amax;
-                named_sync(1 + kGroups, kSoftmaxThreads);
-#pragma unroll
-                for (int u = 0; u < 4 * kGroups; ++u) amax = max(amax, wmax_s[u]);
+                named_sync(kAll, kSoftmaxThreads);
+                amax = __reduce_max_sync(0xffffffffu, lane < 4 * kGroups ? wmax_s[lane] : 0u);
                 // the power of two that brings the largest magnitude into [128, 256); NaN or Inf in q: none, the result is NaN
                 int shift = 0;
                 if (amax > 0 && amax < 0x7F80u) shift = 7 - ((int)(amax >> 7) - 127);
                 shift = max(-100, min(100, shift));
-                const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
-                scale = p.scale_log2 * __uint_as_float((uint32_t)(127 - shift) << 23);
-#pragma unroll
-                for (int u = 0; u < kMine; ++u) {
-                    const int ch = stid + u * kSoftmaxThreads;
-                    if (ch >= n_chunks) continue;
-                    const int r = D == 128 ? ch >> 4 : ch >> 3, c = ch & (per_row - 1);
-                    const uint32_t w[4] = {qv[u].x, qv[u].y, qv[u].z, qv[u].w};
+                const float up = pow2(shift);
+                scale = p.scale_log2 * pow2(-shift);
+#pragma unroll 1
+                for (int ch = stid, u = 0; ch < n_chunks; ch += kSoftmaxThreads, ++u) {
+                    const uint4 x = u == 0 ? qv[0] : u == 1 ? qv[1] : load(ch);
+                    const int r = ch >> per_log2, c = ch & ((1 << per_log2) - 1);
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
                     uint32_t hd[4], rs[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -691,235 +831,260 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 if (lane == 0) mbar_arrive(q_full);
             }
 
-            float l[kC * 8];
+            float l[kC * kEach];
 #pragma unroll
-            for (int k = 0; k < kC * 8; ++k) l[k] = 0.f;
-            for (int c = lane; c < n_c * 8; c += 32) my_sums[c] = my_sums[4 * NP + c] = 0.f;
-            int l_cat = -1;                             // whose sums l holds: 0 outside, 1 inside the span, -1 none
+            for (int k = 0; k < kC * kEach; ++k) l[k] = 0.f;
+            for (int c = lane; c < kC * 8; c += 32) my_sums[c] = my_sums[4 * NP + c] = 0.f;
+            bool l_in = false;                          // l holds sums of positions inside the span
             int k0 = 0;                                 // V scales are taken relative to 2^k0
             float inv_k0 = 1.f;
 
-            // adds this thread's values to the sums of their kind, over the warp
-            auto flush = [&](int cat, bool mine) {
-#pragma unroll
-                for (int c = 0; c < kC; ++c) {
-                    if (c >= n_c) break;
-                    float v[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = mine ? l[c * 8 + k] : 0.f;
-                    const float t = sum8(v, lane);
-                    if ((lane & 3) == 0) my_sums[cat * 4 * NP + c * 8 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1)] += t;
-                }
-                __syncwarp();
+            // adds what the threads hold to the warp's sums
+            auto add_to_sums = [&](int c, float t, bool all, bool in) {
+                if (lane & 3) return;
+                float *at = my_sums + c * 8 + ((lane >> 4) & 1) * 4 + ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1);
+                if (all) *at += t;
+                if (in) at[4 * NP] += t;
             };
-
-            for (int j = 0; j < seg.T; ++j, ++n) {
+            const int j_first = stream;
+            int last = -1;                              // this stream's last tile
+#pragma unroll 1
+            for (int j = j_first;; j += kStreams) {
+                // sums of one kind at a time: a tile inside the span, or another (what one of both has inside is added below)
                 const int pos0 = (seg.t0 + j) * kTilePos, pos = pos0 + row;
-                ks = ks_next;
-                vs = vs_next;
-                scales(e_next, off_next, ks_next, vs_next);
-                at.next_tile(p);
-                e_next = entry();
-                off_next = at.off;
+                const bool inside = pos0 >= vis0 && pos0 + kTilePos <= vis1;
+                if (__builtin_expect(inside != l_in || j >= seg.T, 0)) {
+#pragma unroll
+                    for (int c = 0; c < kC; ++c)
+                        add_to_sums(c, warp_sums<kEach>(l + c * kEach, lane), true, l_in);
+#pragma unroll
+                    for (int k = 0; k < kC * kEach; ++k) l[k] = 0.f;
+                    __syncwarp();
+                    l_in = inside;
+                    if (j >= seg.T) break;
+                }
+                const int n = n0 + j;
                 const bool tail = pos0 + kTilePos > L - gamma;        // some query does not see some position
-                const Seen seen = seen_by(pos - (L - gamma), G, gamma, p.branch_len);
-                const float ck = scale * ks;
+                const bool begins = j == j_first;
+                const uint32_t s_addr = tm_s + place(n, sm.s_log2) * NP + lane_addr + col0;
 
-                mbar_wait(s_full(sr.idx), sr.parity, abort_flag);
+                wait(sc_full(n), round_of(n, sm.s_log2), abort_flag);
+                const float *sc = scale_s + place(n, sm.s_log2) * 16 + (row >> p.block_log2);
+                const float ck = scale * sc[0], vs = sc[8];
+                const int ve = (int)((__float_as_uint(vs) >> 23) & 0xFFu) - 127;
+                if (n >> sm.p_log2) wait(pv_done(n), round_of(n, sm.p_log2) ^ 1u, abort_flag);
+                wait(s_full(n), round_of(n, sm.s_log2), abort_flag);
                 __syncwarp();
                 tc_fence_after();
-                uint32_t raw[kC][8];
-#pragma unroll
-                for (int c = 0; c < kC; ++c)
-                    if (c < n_c) tmem_ld_x8(tm_s + sr.idx * NP + lane_addr + col0 + c * 8, raw[c]);
-                tmem_wait_ld();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(s_free(sr.idx));
-                sr.next(kBufs);
-                float x[kC * 8];
-
-                if (j == 0) {
-                    // the first position's scores set the references
-                    if (row == 0) {
-#pragma unroll
-                        for (int c = 0; c < kC; ++c)
-                            if (c < n_c)
+                if (__builtin_expect(begins, 0)) {
+                    // the first position's scores set the references, its block's V scale the scales'
+                    if (wq == 0) {
+#pragma unroll 1
+                        for (int c = 0; c < kC; ++c) {
+                            uint32_t r[8];
+                            tmem_ld_x8(s_addr + c * 8, r);
+                            tmem_wait_ld();
+                            if (lane == 0)
 #pragma unroll
                                 for (int k = 0; k < 8; ++k) {
-                                    const float y = __uint_as_float(raw[c][k]) * ck;
-                                    m_s[col0 + c * 8 + k] = fabsf(y) < INFINITY ? y - kFirst : 0.f;
+                                    const float y = __uint_as_float(r[k]) * ck;
+                                    nm[c * 8 + k] = fabsf(y) < INFINITY ? kFirst - y : 0.f;
                                 }
-                        const uint32_t e = (__float_as_uint(vs) >> 23) & 0xFFu;
-                        wmax_s[8 + grp] = e > 0 && e < 255 ? e : 127;
+                        }
+                        if (lane == 0) wmax_s[4 * kGroups + grp] = (uint32_t)(ve > -127 && ve < 128 ? max(-100, min(100, ve)) + 127 : 127);
                     }
                     named_sync(bar_id, 128);
-                    k0 = (int)wmax_s[8 + grp] - 127 + 2;
-                    inv_k0 = ldexpf(1.f, -k0);
+                    k0 = (int)wmax_s[4 * kGroups + grp] - 127 + 2;
+                    inv_k0 = pow2(-k0);
                 }
-                float vsr = vs * inv_k0;
-                float gmax = -INFINITY;
-#pragma unroll
-                for (int c = 0; c < kC; ++c)
-                    if (c < n_c) {
-                        const float4 ma = *reinterpret_cast<const float4 *>(m_s + col0 + c * 8);
-                        const float4 mb = *reinterpret_cast<const float4 *>(m_s + col0 + c * 8 + 4);
-                        const float mm[8] = {ma.x, ma.y, ma.z, ma.w, mb.x, mb.y, mb.z, mb.w};
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            float y = fmaf(__uint_as_float(raw[c][k]), ck, -mm[k]);
-                            if (tail) y = seen(col0 + c * 8 + k) ? y : -INFINITY;
-                            x[c * 8 + k] = y;
-                            gmax = fmaxf(gmax, y);
-                        }
+                uint8_t *prow = gbase + sm.p + place(n, sm.p_log2) * (NP * 256) + c_lo * 2048 + row * 16;
+                // A pass is taken back and made again when a score passes the guard, a V scale is large against 2^k0, or the
+                // stream begins in the draft slots, where its first position need not be one that every query sees.
+#pragma unroll 1
+                for (int turn = 0, back = 0;;) {
+                    float top;
+                    const float vsr = vs * inv_k0, sign = back ? -1.f : 1.f;
+                    if (__builtin_expect(!tail, 1)) {
+                        const Seen all = {0, 0xFFFFFFFFu};
+                        top = softmax_pass<kC, kHalf, false>(s_addr, nm, ck, vsr, all, col0, prow, lane, sign, l);
+                    } else {
+                        const Seen seen = seen_by(pos - (L - gamma), G, gamma, p.branch_len);
+                        top = softmax_pass<kC, kHalf, true>(s_addr, nm, ck, vsr, seen, col0, prow, lane, sign, l);
                     }
-                // (a first tile in the draft slots: its first position need not be one that every query sees)
-                if (group_any(bar_id, gmax > kGuard || fabsf(vsr) > 2.f || (j == 0 && tail))) {
-                    // ---- references up to this tile's maxima
-                    uint32_t e = (__float_as_uint(vs) >> 23) & 0xFFu;
-                    if (e == 255u) e = 0u;
-                    e = __reduce_max_sync(0xffffffffu, e);
-#pragma unroll
-                    for (int c = 0; c < kC; ++c)
-                        if (c < n_c)
+                    if (!back) {
+                        const bool beyond = top > kGuard || (ve > k0 && ve < 100) || (begins && tail && turn == 0);
+                        if (__builtin_expect(!group_any(bar_id, beyond) || turn == 3, 1)) break;
+                        // this tile's maxima over the lanes
+                        const Seen seen = seen_by(pos - (L - gamma), G, gamma, p.branch_len);
+                        const int e = __reduce_max_sync(0xffffffffu, ve < 128 ? min(ve, 100) : -127);
+#pragma unroll 1
+                        for (int c = 0; c < kC; ++c) {
+                            uint32_t r[8];
+                            tmem_ld_x8(s_addr + c * 8, r);
+                            tmem_wait_ld();
+                            float x[8];
+                            scores8<true>(r, nm + c * 8, ck, seen, col0 + c * 8, x);
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
-                                const float y = warp_max_f32(x[c * 8 + k]);
-                                if (lane == 0) tmx_s[wq * NP + col0 + c * 8 + k] = y;
+                                const float y = warp_max_f32(x[k]);
+                                if (lane == 0) tmx[wq * NP + c * 8 + k] = y;
                             }
-                    if (lane == 0) wmax_s[warp - kSoftmaxWarp0] = e;
+                        }
+                        if (lane == 0) wmax_s[warp - kSoftmaxWarp0] = (uint32_t)(e + 127);
+                        back = 1;
+                        ++turn;
+                        continue;
+                    }
+                    // ---- the sums are without this tile again: references up to its maxima
+                    named_sync(bar_id, 128);
+                    const int e = (int)__reduce_max_sync(0xffffffffu, wmax_s[grp * 4 + (lane & 3)]) - 127;
+                    const int k_new = e > k0 ? e + 2 : k0;
+                    const float fk = pow2(max(k0 - k_new, -126));
+                    if (gtid < kC * 8) {
+                        const float t = fmaxf(fmaxf(tmx[gtid], tmx[NP + gtid]), fmaxf(tmx[2 * NP + gtid], tmx[3 * NP + gtid]));
+                        const float up = (begins ? t > -INFINITY : t > kGuard) ? t - kFirst : 0.f;
+                        nm[gtid] -= up;
+                        fac[gtid] = ex2(-up);
+                    }
                     named_sync(bar_id, 128);
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) e = max(e, wmax_s[grp * 4 + u]);
-                    const int k_new = (int)e - 127 > k0 ? (int)e - 127 + 2 : k0;
-                    const float fk = j > 0 ? ldexpf(1.f, max(k0 - k_new, -200)) : 1.f;
-                    if (j > 0) {
-                        // (the products of the tile before have ended)
-                        mbar_wait(pv_done(done.idx), done.parity, abort_flag);
+                    for (int c = 0; c < kC; ++c)
+#pragma unroll
+                            for (int k = 0; k < kEach; ++k) {
+                                // (NaN: the tile had brought an infinity, against which what was there before does not count)
+                                const float y = l[c * kEach + k];
+                                l[c * kEach + k] = y == y ? y * fac[c * 8 + (kHalf ? (lane >> 4) * 4 : 0) + k] : 0.f;
+                            }
+                    if (!begins) {
+                        // (the products of the stream's last tile have ended; the next are those of this one)
+                        wait(pv_done(last), round_of(last, sm.p_log2), abort_flag);
                         __syncwarp();
                         tc_fence_after();
-                    }
-#pragma unroll
-                    for (int c = 0; c < kC; ++c)
-                        if (c < n_c) {
+#pragma unroll 1
+                        for (int c = 0; c < kC; ++c) {
+                            const uint32_t o_addr = tm_o + stream * NP + lane_addr + col0 + c * 8;
                             uint32_t o[8];
-                            if (j > 0) {
-                                tmem_ld_x8(tm_o + lane_addr + col0 + c * 8, o);
-                                tmem_wait_ld();
-                            }
+                            tmem_ld_x8(o_addr, o);
+                            tmem_wait_ld();
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const int col = col0 + c * 8 + k;
-                                const float top = fmaxf(fmaxf(tmx_s[col], tmx_s[NP + col]), fmaxf(tmx_s[2 * NP + col], tmx_s[3 * NP + col]));
-                                const bool moves = j == 0 ? top > -INFINITY : top > kGuard;
-                                const float up = moves ? top - kFirst : 0.f;
-                                x[c * 8 + k] -= up;
-                                const float f = ex2(-up);
-                                if (moves) l[c * 8 + k] *= f;
-                                if (j > 0) o[k] = __float_as_uint(__uint_as_float(o[k]) * (f * fk));
-                            }
-                            if (j > 0) tmem_st_x8(tm_o + lane_addr + col0 + c * 8, o);
+                            for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * (fac[c * 8 + k] * fk));
+                            tmem_st_x8(o_addr, o);
                         }
-                    if (j > 0) tmem_wait_st();
-                    tc_fence_before();
-                    // the warp's own sums, and (one warp of the group) the references
-                    for (int c = lane; c < n_c * 8; c += 32) {
-                        const int col = col0 + c;
-                        const float top = fmaxf(fmaxf(tmx_s[col], tmx_s[NP + col]), fmaxf(tmx_s[2 * NP + col], tmx_s[3 * NP + col]));
-                        const bool moves = j == 0 ? top > -INFINITY : top > kGuard;
-                        if (moves) {
-                            const float f = ex2(kFirst - top);
-                            my_sums[c] *= f;
-                            my_sums[4 * NP + c] *= f;
-                            if (wq == 0) m_s[col] += top - kFirst;
-                        }
+                        tmem_wait_st();
                     }
+                    for (int c = lane; c < kC * 8; c += 32) {
+                        my_sums[c] *= fac[c];
+                        my_sums[4 * NP + c] *= fac[c];
+                    }
+                    __syncwarp();
                     k0 = k_new;
-                    inv_k0 = ldexpf(1.f, -k0);
-                    vsr = vs * inv_k0;
-                    named_sync(bar_id, 128);
+                    inv_k0 = pow2(-k0);
+                    back = 0;
                 }
-
-                // ---- probabilities
-                const int cat = pos0 >= vis0 && pos0 + kTilePos <= vis1 ? 1 : pos0 + kTilePos <= vis0 || pos0 >= vis1 ? 0 : 2;
-                if (cat != l_cat) {
-                    if (l_cat >= 0) {
-                        flush(l_cat, true);
+                if (__builtin_expect(!inside && pos0 + kTilePos > vis0 && pos0 < vis1, 0)) {
+                    const Seen seen = seen_by(pos - (L - gamma), G, gamma, p.branch_len);
+                    const bool in = pos >= vis0 && pos < vis1;
+#pragma unroll 1
+                    for (int c = 0; c < kC; ++c) {
+                        uint32_t r[8];
+                        tmem_ld_x8(s_addr + c * 8, r);
+                        tmem_wait_ld();
+                        float x[8];
+                        scores8<true>(r, nm + c * 8, ck, seen, col0 + c * 8, x);
 #pragma unroll
-                        for (int k = 0; k < kC * 8; ++k) l[k] = 0.f;
+                        for (int k = 0; k < 8; ++k) x[k] = in ? ex2(x[k]) : 0.f;
+                        add_to_sums(c, warp_sums<8>(x, lane), false, true);
                     }
-                    l_cat = cat;
+                    __syncwarp();
                 }
-                if (n >= kBufs) mbar_wait(pv_done(br.idx), br.parity ^ 1u, abort_flag);
-                uint8_t *prow = gbase + sm.p + br.idx * (NP * 256) + c_lo * 2048 + row * 16;
-#pragma unroll
-                for (int c = 0; c < kC; ++c)
-                    if (c < n_c) {
-                        float e[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            e[k] = ex2(x[c * 8 + k]);
-                            l[c * 8 + k] += e[k];
-                        }
-                        *reinterpret_cast<uint4 *>(prow + c * 2048) =
-                            make_uint4(pack_f16x2(e[0] * vsr, e[1] * vsr), pack_f16x2(e[2] * vsr, e[3] * vsr),
-                                       pack_f16x2(e[4] * vsr, e[5] * vsr), pack_f16x2(e[6] * vsr, e[7] * vsr));
-                    }
+                tc_fence_before();
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(br.idx));
-                done = br;
-                br.next(kBufs);
-                if (cat == 2) {
-                    const bool in = pos >= vis0 && pos < vis1;
-                    flush(1, in);
-                    flush(0, !in);
-#pragma unroll
-                    for (int k = 0; k < kC * 8; ++k) l[k] = 0.f;
-                    l_cat = -1;
+                if (lane == 0) {
+                    mbar_arrive(p_full(n));
+                    mbar_arrive(s_free(n));
                 }
+                last = n;
             }
-            if (l_cat >= 0) flush(l_cat, true);
-            mbar_wait(pv_done(done.idx), done.parity, abort_flag);
+            n0 += seg.T;
+            if (last >= 0) wait(pv_done(last), round_of(last, sm.p_log2), abort_flag);
             __syncwarp();
             tc_fence_after();
-            named_sync(bar_id, 128);                    // the group's sums are there
+            if (gtid == 0) wmax_s[4 * kGroups + grp] = (uint32_t)(k0 + 1024);
+            named_sync(kAll, kSoftmaxThreads);             // all sums are there
 
-            // ---- results: whole, or this CTA's part of them
+            // ---- a row's weights: each stream's part of the sum, in fac_s
             const bool whole = seg.first && seg.last;
-            const float vk = ldexpf(1.f, k0 / 2), vk2 = ldexpf(1.f, k0 - k0 / 2);
             const int slot = part_slot(blockIdx.x, seg.first);
             float *part_o = p.part_o + (size_t)slot * M * D;
-            float *part_stat = p.part_stat + (size_t)slot * M * 4;
-#pragma unroll 1
-            for (int c = 0; c < n_c; ++c) {
-                uint32_t o[8];
-                tmem_ld_x8(tm_o + lane_addr + col0 + c * 8, o);
-                tmem_wait_ld();
+            if (stid < M) {
+                const int col = stid;
+                float all[kStreams], in[kStreams], m[kStreams], top = -INFINITY;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int col = col0 + c * 8 + k;
-                    if (col >= M) break;
-                    const float *t = sums_s + col;
-                    const float in = t[4 * NP] + t[5 * NP] + t[6 * NP] + t[7 * NP];
-                    const float all = t[0] + t[NP] + t[2 * NP] + t[3 * NP] + in;
-                    const float v = __uint_as_float(o[k]) * vk * vk2;
+                for (int u = 0; u < kStreams; ++u) {
+                    const float *t = sums_s + u * 8 * NP + col;
+                    in[u] = t[4 * NP] + t[5 * NP] + t[6 * NP] + t[7 * NP];
+                    all[u] = t[0] + t[NP] + t[2 * NP] + t[3 * NP];
+                    m[u] = -nm_s[u * NP + col];
+                    if (all[u] != 0.f) top = fmaxf(top, m[u]);
+                }
+                float total = 0.f, vis = 0.f, w[kStreams];
+#pragma unroll
+                for (int u = 0; u < kStreams; ++u) {
+                    w[u] = all[u] != 0.f ? ex2(m[u] - top) : 0.f;     // (a stream without tiles, or that the row sees nothing of)
+                    if (w[u] != 0.f) {
+                        total = fmaf(w[u], all[u], total);
+                        vis = fmaf(w[u], in[u], vis);
+                    }
+                }
+                const float inv = total == 0.f ? 0.f : 1.f / total;   // a query that sees nothing gives zeros
+#pragma unroll
+                for (int u = 0; u < kStreams; ++u) {
+                    const int g_of = u * kShare + col / (8 * kC);       // the group of this stream that has the column
+                    fac_s[u * NP + col] = (whole ? w[u] * inv : w[u]) * pow2((int)wmax_s[4 * kGroups + g_of] - 1024);
+                }
+                const int g = div_by(col, G, P.group_magic), hg = col - g * G;
+                const int out_row = (seg.b * gamma + g) * p.Hq + seg.head * G + hg;
+                row_s[col] = out_row;
+                if (whole) {
+                    p.mass[out_row] = vis * inv;
+                } else {
+                    *reinterpret_cast<float4 *>(p.part_stat + ((size_t)slot * M + col) * 4) = make_float4(top, total, vis, 0.f);
+                }
+            }
+            named_sync(kAll, kSoftmaxThreads);
+            // ---- results: whole, or this CTA's part of them; the chunks of columns go to the groups in turn
+            if (row < D) {
+#pragma unroll 1
+                for (int c = grp; c * 8 < M; c += kGroups) {
+                    float v[8] = {};
+#pragma unroll
+                    for (int u = 0; u < kStreams; ++u) {
+                        uint32_t o[8];
+                        tmem_ld_x8(tm_o + u * NP + lane_addr + c * 8, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float w = fac_s[u * NP + c * 8 + k];
+                            v[k] = w != 0.f ? fmaf(w, __uint_as_float(o[k]), v[k]) : v[k];
+                        }
+                    }
                     if (whole) {
-                        const int g = div_by(col, G, P.group_magic), hg = col - g * G;
-                        const size_t at_row = ((size_t)seg.b * gamma + g) * p.Hq + seg.head * G + hg;
-                        const float inv = all == 0.f ? 0.f : 1.f / all;       // a query that sees nothing gives zeros
-                        if (row < D) p.out[at_row * D + row] = (uint16_t)(pack_bf16x2(all == 0.f ? 0.f : v * inv, 0.f) & 0xFFFFu);
-                        if (row == 0) p.mass[at_row] = in * inv;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (c * 8 + k < M) p.out[(size_t)row_s[c * 8 + k] * D + row] = (uint16_t)(pack_bf16x2(v[k], 0.f) & 0xFFFFu);
                     } else {
-                        if (row < D) part_o[(size_t)col * D + row] = v;
-                        if (row == 0) *reinterpret_cast<float4 *>(part_stat + col * 4) = make_float4(m_s[col], all, in, 0.f);
+                        float *to = part_o + c * 8 * D + row;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (c * 8 + k < M) to[k * D] = v[k];
                     }
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(o_free);
-            named_sync(1 + kGroups, kSoftmaxThreads);   // sums, references and q may be written anew
+            named_sync(kAll, kSoftmaxThreads);             // sums, references and q may be written anew
         }
     }
     __syncwarp();
@@ -942,7 +1107,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_paged_fp8_kernel(const
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_launch_dependents();
     grid_dependency_wait();
-    if (warp == 0) make_line(line, p);
+    if (warp == 0) make_line(line, p.kv_len, p.B, p.Hkv, p.max_len, p.n_cta);
     __syncthreads();
     const int row = blockIdx.x * kMergeWarps + warp;
     if (row >= p.B * p.gamma * p.Hq) return;
@@ -1024,13 +1189,14 @@ bool make_pool_map(CUtensorMap *map, const uint8_t *pool, const PagedFp8Params &
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kC>
+template <int kStreams, int kC, bool kHalf>
 cudaError_t launch_attention(const KernelParams &P, const CUtensorMap &tk, const CUtensorMap &tv, cudaStream_t stream, int *launches)
 {
     const size_t smem = P.sm.total + 1024;
-    cudaError_t e = cudaFuncSetAttribute(attn_paged_fp8_kernel<kC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = cudaFuncSetAttribute(attn_paged_fp8_kernel<kStreams, kC, kHalf>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_after(attn_paged_fp8_kernel<kC>, dim3((unsigned)P.a.n_cta), kThreads, smem, P.a.pdl != 0, stream, launches, P, tk, tv);
+    return launch_after(attn_paged_fp8_kernel<kStreams, kC, kHalf>, dim3((unsigned)P.a.n_cta), kThreads, smem, P.a.pdl != 0, stream,
+                        launches, P, tk, tv);
 }
 
 }  // namespace
@@ -1042,26 +1208,30 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
 {
     KernelParams P;
     P.a = p;
-    P.NP = (p.M + 15) & ~15;
+    P.NP = p.M > 96 ? 128 : (p.M + 15) & ~15;
+    // as many streams as tensor memory holds accumulators for, beside 2 x 64 columns of V^T and the S^T buffers
+    const int streams = P.NP <= 32 ? 4 : P.NP <= 96 ? 2 : 1;
+    const int s_log2 = kVBufs * 64 + (streams + 4) * P.NP <= 512 ? 2 : 1, p_log2 = P.NP <= 64 ? 2 : 1;
     int cols = 32;
-    while (cols < kBufs * 64 + (kBufs + 1) * P.NP) cols *= 2;
+    while (cols < kVBufs * 64 + (streams + (1 << s_log2)) * P.NP) cols *= 2;
     P.tmem_cols = cols;
     P.group_magic = p.G > 1 ? 0xFFFFFFFFu / (uint32_t)p.G + 1u : 0u;
     // as many slots as shared memory holds, K's one more where the count is odd (its tile is used first)
     int slots = 12;
-    do P.sm = smem_map(p.D, P.NP, (slots + 1) / 2, slots / 2);
+    do P.sm = smem_map(p.D, P.NP, streams, (slots + 1) / 2, slots / 2, s_log2, p_log2);
     while (P.sm.total + 1024 > 227 * 1024 && --slots > 2);
     CUtensorMap tk, tv;
     if (!make_pool_map(&tk, k_pool, p) || !make_pool_map(&tv, v_pool, p)) return cudaErrorInvalidValue;
     cudaError_t e;
-    switch ((((p.M + 7) / 8) + 1) / 2) {
-        case 1: e = launch_attention<1>(P, tk, tv, stream, launches); break;
-        case 2: e = launch_attention<2>(P, tk, tv, stream, launches); break;
-        case 3: e = launch_attention<3>(P, tk, tv, stream, launches); break;
-        case 4: e = launch_attention<4>(P, tk, tv, stream, launches); break;
-        case 5: e = launch_attention<5>(P, tk, tv, stream, launches); break;
-        case 6: e = launch_attention<6>(P, tk, tv, stream, launches); break;
-        default: e = launch_attention<8>(P, tk, tv, stream, launches); break;
+    switch (P.NP / 16) {
+        case 1: e = p.M <= 8 ? launch_attention<4, 1, false>(P, tk, tv, stream, launches)
+                             : launch_attention<4, 2, false>(P, tk, tv, stream, launches); break;
+        case 2: e = launch_attention<4, 4, false>(P, tk, tv, stream, launches); break;
+        case 3: e = launch_attention<2, 3, false>(P, tk, tv, stream, launches); break;
+        case 4: e = launch_attention<2, 4, false>(P, tk, tv, stream, launches); break;
+        case 5: e = launch_attention<2, 5, true>(P, tk, tv, stream, launches); break;
+        case 6: e = launch_attention<2, 6, true>(P, tk, tv, stream, launches); break;
+        default: e = launch_attention<1, 4, true>(P, tk, tv, stream, launches); break;
     }
     if (e != cudaSuccess) return e;
     const int rows = p.B * p.gamma * p.Hq;
