@@ -45,12 +45,12 @@ namespace {
 using namespace ptx;
 
 constexpr int kTilePos = 128;
-constexpr int kConvertWarp0 = 4, kSoftmaxWarp0 = 8;
+constexpr int kVBufs = 2;                   // V^T buffers in tensor memory, and sets of four warps that fill them
+constexpr int kConvertWarp0 = 4, kSoftmaxWarp0 = kConvertWarp0 + 4 * kVBufs;
 constexpr int kGroups = 4;                  // softmax groups of four warps
 constexpr int kSoftmaxThreads = 128 * kGroups;
 constexpr int kThreads = 32 * kSoftmaxWarp0 + kSoftmaxThreads;
 constexpr int kMergeWarps = 8;
-constexpr int kVBufs = 2;                   // V^T buffers in tensor memory
 constexpr int kMaxBufs = 4;                 // S^T buffers and P^T buffers, at most
 constexpr float kFirst = 3.f;               // log2 of the probability of a stream's first position
 constexpr float kGuard = 14.f;              // log2 units above the reference before it moves
@@ -82,7 +82,7 @@ __device__ __forceinline__ int ceil_div(int x, int d, uint32_t m)
 __device__ __forceinline__ uint32_t magic_of(uint32_t d) { return d > 1 ? 0xFFFFFFFFu / d + 1u : 0u; }
 
 // One warp.  True when a length lies outside 0..max_len (the sequence then counts as empty).
-__device__ __noinline__ bool make_line(Line &w, const int32_t *kv_len, int B, int Hkv, int max_len, int n_cta)
+__device__ __forceinline__ bool make_line(Line &w, const int32_t *kv_len, int B, int Hkv, int max_len, int n_cta)
 {
     const int lane = threadIdx.x & 31;
     int total = 0;
@@ -149,9 +149,7 @@ struct Walk {
         end = min(at + w.share, w.start[n_seq]);
     }
 };
-// (out of line: six roles step through their segments, and what counts in this kernel is that its loops stay in the
-// instruction caches)
-__device__ __noinline__ bool next_segment(const Line &w, Walk &walk, Segment &s)
+__device__ __forceinline__ bool next_segment(const Line &w, Walk &walk, Segment &s)
 {
     if (walk.at >= walk.end) return false;
     int b = walk.b;
@@ -329,19 +327,21 @@ __device__ __forceinline__ void ldmatrix_b8_x2(uint32_t addr, uint32_t (&r)[4])
     asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-// 16 lanes x 64 columns: lane t's registers 4 i .. 4 i + 3 are row t / 4, columns 8 i + 2 (t % 4) and the next,
+// 16 lanes x 32 columns: lane t's registers 4 i .. 4 i + 3 are row t / 4, columns 8 i + 2 (t % 4) and the next,
 // then row t / 4 + 8.
-__device__ __forceinline__ void tmem_st_16x256b_x8(uint32_t taddr, const uint32_t (&r)[32])
+__device__ __forceinline__ void tmem_st_16x256b_x4(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.16x256b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+// Takes registers from (gives them to) the pool that the block was launched with.
+template <int kRegs>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs) : "memory"); }
+template <int kRegs>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
 // D[tmem] (+)= A[tmem] * B[smem desc]
 __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
 {
@@ -385,6 +385,13 @@ __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b)
     return r;
 }
 __device__ __forceinline__ uint64_t pair(float lo, float hi) { return pack_f32x2(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // Scaled scores x of eight columns: score * ck + (minus the reference)
 template <bool kMask>
 __device__ __forceinline__ void scores8(const uint32_t *raw, const float *nm, float ck, Seen seen, int col, float (&x)[8])
@@ -424,7 +431,7 @@ __device__ __forceinline__ float softmax_pass(uint32_t s_addr, const float *nm, 
         if (c + 1 < kC) tmem_ld_x8(s_addr + (c + 1) * 8, raw[(c + 1) & 1]);
         float x[8];
         scores8<kMask>(raw[c & 1], nm + c * 8, ck, seen, col0 + c * 8, x);
-        top = fmaxf(top, fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))));
+        top = max3(max3(top, x[0], x[1]), max3(x[2], x[3], x[4]), max3(x[5], x[6], x[7]));
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = ex2(x[k]);
         if constexpr (kHalf) {
@@ -506,7 +513,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
             const int j = i - 2 * (sm.ks + sm.vs);
             uint32_t count = 1;
             if (j < 0) count = i >= 2 * sm.ks + sm.vs ? D / 32 : 1;                             // v_empty: the converting warps
-            else if (j >= kMaxBufs && j < 3 * kMaxBufs) count = 4 * kShare;                     // s_free, p_full
+            else if (j >= kMaxBufs && j < 3 * kMaxBufs) count = kShare;                         // s_free, p_full: one thread of a group
             else if (j >= 5 * kMaxBufs && j < 5 * kMaxBufs + kVBufs) count = D / 32;            // vt_full
             else if (j == 5 * kMaxBufs + 2 * kVBufs || j == 5 * kMaxBufs + 2 * kVBufs + 1) count = 4 * kGroups;     // q_full, o_free
             mbar_init(bar0 + 8 * i, count);
@@ -539,8 +546,12 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
     Walk walk(line, p.B, blockIdx.x);
     Segment seg;
 
+    // Registers go from the warps that issue and convert to those of the softmax, which keep their sums in them:
+    // 4 x 32 x 40 + 8 x 32 x 48 + 16 x 32 x 88 = 62464 of the launch's 28 x 32 x 72 = 64512.
+    static_assert(32 * (4 * 40 + 4 * kVBufs * 48 + 4 * kGroups * 88) <= kThreads * 72 && kThreads * 72 <= 65536, "register pool");
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer
+        fewer_registers<40>();
         const uint64_t policy = l2_evict_first_policy();
         Ring kr, vr;
         const int boxes = p.page_size < kTilePos ? kTilePos / p.page_size : 1;
@@ -592,6 +603,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ K.Q^T issuer
+        fewer_registers<40>();
         const uint32_t idesc = make_idesc_e4m3(128, NP, 0, 0);
         const uint32_t swz = D == 128 ? kSwizzle128B : kSwizzle64B;
         const uint64_t kd0 = make_smem_desc(base + sm.k, 16, 8 * D, swz), qd0 = make_smem_desc(base + sm.q, 16, 8 * D, swz);
@@ -632,6 +644,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         __syncwarp();
     } else if (warp == 2) {
         // ------------------------------------------------------------ P.V issuer
+        fewer_registers<40>();
         const uint32_t idesc = make_idesc_f16(128, NP, 1);
         const uint64_t pd0 = make_smem_desc(base + sm.p, 128, 2048, kSwizzleNone);
         Ring vr, orr;
@@ -668,59 +681,65 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         __syncwarp();
     } else if (warp >= kConvertWarp0 && warp < kSoftmaxWarp0) {
         // ------------------------------------------------- V codes to fp16 in tensor memory
+        fewer_registers<48>();
         const int wq = warp & 3;                       // channels 32 wq .. + 31 = TMEM lanes
-        Ring vr, br;
+        const int set = (warp - kConvertWarp0) >> 2;   // tiles set, set + kVBufs, ... into V^T buffer `set`
+        Ring vr;
+        for (int i = 0; i < set; ++i) vr.next(sm.vs);
+        uint32_t parity = 0;
         int n = 0;
         bool ok = 32 * wq < D;
         while (ok && next_segment(line, walk, seg)) {
-            for (int j = 0; ok && j < seg.T; ++j, ++n) {
+            int j = (set - n) & (kVBufs - 1);
+            n += seg.T;
+#pragma unroll 1
+            for (; j < seg.T; j += kVBufs) {
                 ok = wait(v_full(vr.idx), vr.parity, abort_flag);
-                if (n >= kVBufs) ok = wait(vt_free(br.idx), br.parity ^ 1u, abort_flag) && ok;
+                ok = wait(vt_free(set), parity ^ 1u, abort_flag) && ok;       // (at once for the first tile)
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 const int live = seg.len - (seg.t0 + j) * kTilePos;      // positions of this tile below the length
                 const uint32_t tile = base + sm.v + vr.idx * slot_bytes;
+                // 16 channels x 64 positions a turn
+                const uint32_t from = tile + lane * D, to = tm_v + set * 64 + ((uint32_t)(wq * 32) << 16);
+                const int phase = D == 128 ? lane & 7 : (lane >> 1) & 3;
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t r[4][4], w[32];
+                for (int h = 0; h < 4; ++h) {
+                    const int chunk = wq * 2 + (h & 1), half = h >> 1;
+                    uint32_t r[2][4], w[16];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int pos = u * 32 + lane, chunk = wq * 2 + h;
-                        const int phase = D == 128 ? pos & 7 : (pos >> 1) & 3;
-                        ldmatrix_b8_x2(tile + pos * D + ((chunk ^ phase) << 4), r[u]);
-                    }
+                    for (int u = 0; u < 2; ++u) ldmatrix_b8_x2(from + (half * 2 + u) * 32 * D + ((chunk ^ phase) << 4), r[u]);
                     if (__builtin_expect(live < kTilePos, 0)) {
                         // what lies behind the sequence is not the cache's: it may be anything, NaN among it
 #pragma unroll
-                        for (int u = 0; u < 4; ++u)
+                        for (int u = 0; u < 2; ++u)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                const int left = live - (u * 32 + (k >> 1) * 16 + (lane & 3) * 4);
+                                const int left = live - (half * 64 + u * 32 + (k >> 1) * 16 + (lane & 3) * 4);
                                 if (left < 4) r[u][k] &= left <= 0 ? 0u : 0xFFFFFFFFu >> (8 * (4 - left));
                             }
                     }
                     // matrix m of a pair holds registers 2 m (row) and 2 m + 1 (row + 8)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) decode4(r[u][k], w[u * 8 + k * 2], w[u * 8 + k * 2 + 1]);
-                    if (h == 1) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(v_empty(vr.idx));
-                    }
-                    tmem_st_16x256b_x8(tm_v + br.idx * 64 + ((uint32_t)(wq * 32 + h * 16) << 16), w);
+                    tmem_st_16x256b_x4(to + half * 32 + ((uint32_t)((h & 1) * 16) << 16), w);
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_empty(vr.idx));
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(vt_full(br.idx));
-                vr.next(sm.vs);
-                br.next(kVBufs);
+                if (lane == 0) mbar_arrive(vt_full(set));
+                for (int i = 0; i < kVBufs; ++i) vr.next(sm.vs);
+                parity ^= 1u;
             }
         }
     } else if (warp == 3) {
         // ------------------------------------------------- the blocks' scales, from global to shared memory
+        fewer_registers<40>();
         // lanes 0..7 the K scales of a tile's blocks, 16..23 the V scales
         const int blk = lane & 15, in_tile = blk << p.block_log2;
         const float *from = lane < 16 ? p.k_scale : p.v_scale;
@@ -756,6 +775,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         }
     } else if (warp >= kSoftmaxWarp0) {
         // ------------------------------------------------------------ softmax
+        more_registers<88>();
         const int grp = (warp - kSoftmaxWarp0) >> 2, bar_id = 1 + grp;
         constexpr int kAll = 1 + kGroups;                       // barrier of all softmax threads
         const int stream = grp / kShare, part = grp % kShare;
@@ -912,6 +932,9 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                         top = softmax_pass<kC, kHalf, true>(s_addr, nm, ck, vsr, seen, col0, prow, lane, sign, l);
                     }
                     if (!back) {
+                        // (all of the group's P^T is on its way to the tensor core when the vote is over)
+                        tc_fence_before();
+                        fence_proxy_async_smem();
                         const bool beyond = top > kGuard || (ve > k0 && ve < 100) || (begins && tail && turn == 0);
                         if (__builtin_expect(!group_any(bar_id, beyond) || turn == 3, 1)) break;
                         // this tile's maxima over the lanes
@@ -995,12 +1018,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                         for (int k = 0; k < 8; ++k) x[k] = in ? ex2(x[k]) : 0.f;
                         add_to_sums(c, warp_sums<8>(x, lane), false, true);
                     }
-                    __syncwarp();
+                    tc_fence_before();
+                    named_sync(bar_id, 128);            // (S^T has been read once more)
                 }
-                tc_fence_before();
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
+                if (gtid == 0) {
                     mbar_arrive(p_full(n));
                     mbar_arrive(s_free(n));
                 }
@@ -1229,9 +1250,9 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
         case 2: e = launch_attention<4, 4, false>(P, tk, tv, stream, launches); break;
         case 3: e = launch_attention<2, 3, false>(P, tk, tv, stream, launches); break;
         case 4: e = launch_attention<2, 4, false>(P, tk, tv, stream, launches); break;
-        case 5: e = launch_attention<2, 5, true>(P, tk, tv, stream, launches); break;
+        case 5: e = launch_attention<2, 5, false>(P, tk, tv, stream, launches); break;
         case 6: e = launch_attention<2, 6, true>(P, tk, tv, stream, launches); break;
-        default: e = launch_attention<1, 4, true>(P, tk, tv, stream, launches); break;
+        default: e = launch_attention<1, 4, false>(P, tk, tv, stream, launches); break;
     }
     if (e != cudaSuccess) return e;
     const int rows = p.B * p.gamma * p.Hq;
