@@ -47,9 +47,25 @@ using namespace ptx;
 constexpr int kTilePos = 128;
 constexpr int kVBufs = 2;                   // V^T buffers in tensor memory, and sets of four warps that fill them
 constexpr int kConvertWarp0 = 4, kSoftmaxWarp0 = kConvertWarp0 + 4 * kVBufs;
-constexpr int kGroups = 4;                  // softmax groups of four warps
-constexpr int kSoftmaxThreads = 128 * kGroups;
-constexpr int kThreads = 32 * kSoftmaxWarp0 + kSoftmaxThreads;
+__host__ __device__ constexpr int threads_of(int groups) { return 32 * kSoftmaxWarp0 + 128 * groups; }      // groups: softmax groups of four warps
+// Registers of a thread at launch, and what the softmax warps are given when the others have given up theirs (kIssueRegs for the
+// four warps that issue, kConvertRegs for those that convert).
+constexpr int kIssueRegs = 40, kConvertRegs = 48;
+__host__ __device__ constexpr int launch_regs(int groups) { return groups == 4 ? 72 : groups == 3 ? 80 : 96; }
+__host__ __device__ constexpr int softmax_regs(int groups) { return groups == 4 ? 88 : groups == 3 ? 112 : 168; }
+// chunks of columns that the registers hold beside the sums
+__host__ __device__ constexpr int block_of(int groups, int chunks)
+{
+    const int room = (softmax_regs(groups) - 36) / 8 - chunks;
+    return room >= chunks ? chunks : room >= (chunks + 1) / 2 ? (chunks + 1) / 2 : room >= 2 ? 2 : 1;
+}
+__host__ __device__ constexpr bool pool_holds(int groups)
+{
+    return 32 * (kConvertWarp0 * kIssueRegs + 4 * kVBufs * kConvertRegs + 4 * groups * softmax_regs(groups)) <=
+               threads_of(groups) * launch_regs(groups) &&
+           threads_of(groups) * launch_regs(groups) <= 65536;
+}
+static_assert(pool_holds(2) && pool_holds(3) && pool_holds(4), "a share of the registers that is not there is waited for without end");
 constexpr int kMergeWarps = 8;
 constexpr int kMaxBufs = 4;                 // S^T buffers and P^T buffers, at most
 constexpr float kFirst = 3.f;               // log2 of the probability of a stream's first position
@@ -172,11 +188,11 @@ __device__ __forceinline__ int part_slot(int cta, bool first) { return 2 * cta +
 
 // ---- shared memory --------------------------------------------------------------------
 struct Smem {
-    uint32_t k, v, q, p, nm, tmx, fac, sums, rows, scale, bars, misc, line, total;
+    uint32_t k, v, q, p, nm, tmx, fac, sums, rows, scale, bars, misc, seg, line, total;
     int ks, vs;                             // K and V slots
     int s_log2, p_log2;                     // S^T and P^T buffers
 };
-constexpr int kBarsFixed = 5 * kMaxBufs + 2 * kVBufs + 4;
+constexpr int kBarsFixed = 3 * kMaxBufs + 2 * kVBufs + 4;
 Smem smem_map(int D, int NP, int streams, int ks, int vs, int s_log2, int p_log2)
 {
     Smem s;
@@ -197,6 +213,7 @@ Smem smem_map(int D, int NP, int streams, int ks, int vs, int s_log2, int p_log2
     s.scale = o; o += kMaxBufs * 16 * 4;    // [S^T buffer][K, V][block of the tile]
     s.bars = o; o += 8 * (2 * ks + 2 * vs + kBarsFixed);
     s.misc = o; o += 128;                   // TMEM address, abort flag, words of the softmax warps and groups
+    s.seg = o; o += (sizeof(Segment) + 15) & ~15u;
     s.line = o; o += (sizeof(Line) + 15) & ~15u;
     s.total = o;
     return s;
@@ -357,19 +374,14 @@ __device__ __forceinline__ constexpr uint32_t make_idesc_f16(uint32_t M, uint32_
 }
 constexpr uint32_t kSwizzle64B = 4;
 
-// Sums of kN (8 or 4) values over the warp's lanes (kN = 4: over those that agree in bit 4, which tells whose four
-// values they are).  Lanes with lane % 4 == 0 get the sum of value number (bits 4, 3, 2 of the lane, or bits 3, 2), the
-// highest bit first: nine (five) shuffles where plain sums take forty (sixteen).
-template <int kN>
+// Sum of each of eight values over the warp's lanes: lanes with lane % 4 == 0 get that of value number (bits 4, 3, 2 of the
+// lane, the highest first).  Nine shuffles where plain sums take forty.
 __device__ __forceinline__ float warp_sums(const float *v, int lane)
 {
     float a[4], b[2], c;
     const bool h16 = lane & 16, h8 = lane & 8, h4 = lane & 4;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (kN == 8) a[k] = (h16 ? v[k + 4] : v[k]) + __shfl_xor_sync(0xffffffffu, h16 ? v[k] : v[k + 4], 16);
-        else a[k] = v[k];
-    }
+    for (int k = 0; k < 4; ++k) a[k] = (h16 ? v[k + 4] : v[k]) + __shfl_xor_sync(0xffffffffu, h16 ? v[k] : v[k + 4], 16);
 #pragma unroll
     for (int k = 0; k < 2; ++k) b[k] = (h8 ? a[k + 2] : a[k]) + __shfl_xor_sync(0xffffffffu, h8 ? a[k] : a[k + 2], 8);
     c = (h4 ? b[1] : b[0]) + __shfl_xor_sync(0xffffffffu, h4 ? b[0] : b[1], 4);
@@ -385,6 +397,24 @@ __device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b)
     return r;
 }
 __device__ __forceinline__ uint64_t pair(float lo, float hi) { return pack_f32x2(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+        "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+          "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float r;
@@ -406,54 +436,63 @@ __device__ __forceinline__ void scores8(const uint32_t *raw, const float *nm, fl
         for (int k = 0; k < 8; ++k) x[k] = seen(col + k) ? x[k] : -INFINITY;
 }
 
-// Sums a thread keeps: of all eight columns of a chunk, or (kHalf, many rows) of four, the other four having gone to the lane
-// 16 away, whose own four come here.
-__device__ __forceinline__ void own4(const float (&e)[8], int lane, float (&t)[4])
+// Eight columns of one position: probabilities into P^T and (times sign, s2) the sums.
+template <bool kMask>
+__device__ __forceinline__ void softmax8(const uint32_t *raw, const float *nm, float ck, Seen seen, int col, uint64_t v2, uint64_t s2,
+                                         float &top, float *l, uint8_t *to)
 {
-    const bool hi = lane & 16;
+    float x[8];
+    scores8<kMask>(raw, nm, ck, seen, col, x);
+    top = max3(max3(top, x[0], x[1]), max3(x[2], x[3], x[4]), max3(x[5], x[6], x[7]));
 #pragma unroll
-    for (int k = 0; k < 4; ++k) t[k] = (hi ? e[k + 4] : e[k]) + __shfl_xor_sync(0xffffffffu, hi ? e[k] : e[k + 4], 16);
+    for (int k = 0; k < 8; ++k) x[k] = ex2(x[k]);
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint64_t e2 = pair(x[2 * k], x[2 * k + 1]);
+        unpack_f32x2(fma_f32x2(s2, e2, pair(l[2 * k], l[2 * k + 1])), l[2 * k], l[2 * k + 1]);
+        float a, b;
+        unpack_f32x2(mul_f32x2(e2, v2), a, b);
+        w[k] = pack_f16x2(a, b);
+    }
+    *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// One tile, one position, up to kC chunks of eight columns: probabilities into P^T and (times sign) the sums; returns the largest
-// scaled score.
-template <int kC, bool kHalf, bool kMask>
+// kN chunks of eight columns, asked for in as few instructions as it takes.
+template <int kN>
+__device__ __forceinline__ void tmem_ld_chunks(uint32_t taddr, uint32_t *r)
+{
+    if constexpr (kN >= 4) {
+        tmem_ld_x32(taddr, *reinterpret_cast<uint32_t(*)[32]>(r));
+        if constexpr (kN > 4) tmem_ld_chunks<kN - 4>(taddr + 32, r + 32);
+    } else if constexpr (kN >= 2) {
+        tmem_ld_x16(taddr, *reinterpret_cast<uint32_t(*)[16]>(r));
+        if constexpr (kN > 2) tmem_ld_chunks<kN - 2>(taddr + 16, r + 16);
+    } else {
+        tmem_ld_x8(taddr, *reinterpret_cast<uint32_t(*)[8]>(r));
+    }
+}
+
+// One tile, one position, kC chunks of eight columns, kBlock of them at a time (asking tensor memory and waiting for it takes
+// 170 cycles, whatever the number of columns; 16 columns' work takes 330): probabilities into P^T and (times sign) the sums;
+// returns the largest scaled score.
+template <int kC, int kBlock, bool kMask>
 __device__ __forceinline__ float softmax_pass(uint32_t s_addr, const float *nm, float ck, float vsr, Seen seen, int col0,
-                                              uint8_t *prow, int lane, float sign, float (&l)[kC * (kHalf ? 4 : 8)])
+                                              uint8_t *prow, float sign, float (&l)[kC * 8])
 {
     float top = -INFINITY;
-    uint32_t raw[2][8];
-    tmem_ld_x8(s_addr, raw[0]);
     const uint64_t v2 = pair(vsr, vsr), s2 = pair(sign, sign);
 #pragma unroll
-    for (int c = 0; c < kC; ++c) {
+    for (int b = 0; b < kC; b += kBlock) {
+        uint32_t raw[8 * kBlock];
+        if (b + kBlock <= kC) tmem_ld_chunks<kBlock>(s_addr + b * 8, raw);
+        else tmem_ld_chunks<kC % kBlock == 0 ? 1 : kC % kBlock>(s_addr + b * 8, raw);
         tmem_wait_ld();
-        if (c + 1 < kC) tmem_ld_x8(s_addr + (c + 1) * 8, raw[(c + 1) & 1]);
-        float x[8];
-        scores8<kMask>(raw[c & 1], nm + c * 8, ck, seen, col0 + c * 8, x);
-        top = max3(max3(top, x[0], x[1]), max3(x[2], x[3], x[4]), max3(x[5], x[6], x[7]));
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = ex2(x[k]);
-        if constexpr (kHalf) {
-            float t[4];
-            own4(x, lane, t);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) l[c * 4 + k] = fmaf(sign, t[k], l[c * 4 + k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint64_t t = fma_f32x2(s2, pair(x[2 * k], x[2 * k + 1]), pair(l[c * 8 + 2 * k], l[c * 8 + 2 * k + 1]));
-                unpack_f32x2(t, l[c * 8 + 2 * k], l[c * 8 + 2 * k + 1]);
-            }
-        }
-        uint32_t w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            float a, b;
-            unpack_f32x2(mul_f32x2(pair(x[2 * k], x[2 * k + 1]), v2), a, b);
-            w[k] = pack_f16x2(a, b);
-        }
-        *reinterpret_cast<uint4 *>(prow + c * 2048) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int u = 0; u < kBlock; ++u)
+            if (b + u < kC)
+                softmax8<kMask>(raw + u * 8, nm + (b + u) * 8, ck, seen, col0 + (b + u) * 8, v2, s2, top, l + (b + u) * 8,
+                                prow + (b + u) * 2048);
     }
     return top;
 }
@@ -465,13 +504,14 @@ __device__ __forceinline__ int div_by(int x, int d, uint32_t m)
     return q * d > x ? q - 1 : q;
 }
 
-// The softmax groups take the tiles in turn, kStreams of them, each with its own references, sums and accumulators of O (a
-// stream), put together when the segment ends; the groups of a stream (4 / kStreams) share out the columns, at most kC chunks of
+// kGroups softmax groups take the tiles in turn, kStreams of them, each with its own references, sums and accumulators of O (a
+// stream), put together when the segment ends; the groups of a stream (kGroups / kStreams) share out the columns, kC chunks of
 // eight to a group.
-template <int kStreams, int kC, bool kHalf>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int kStreams, int kGroups, int kC>
+__global__ void __launch_bounds__(threads_of(kGroups), 1)
 attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v)
 {
+    constexpr int kSoftmaxThreads = 128 * kGroups;
     extern __shared__ uint8_t smem_raw[];
     const PagedFp8Params &p = P.a;
     const Smem &sm = P.sm;
@@ -487,6 +527,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
     volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + sm.misc + 4);
     volatile uint32_t *wmax_s = reinterpret_cast<volatile uint32_t *>(gbase + sm.misc + 16);
     Line &line = *reinterpret_cast<Line *>(gbase + sm.line);
+    volatile Segment &seg_s = *reinterpret_cast<volatile Segment *>(gbase + sm.seg);     // the softmax warps'
     const uint32_t slot_bytes = kTilePos * D;
 
     const uint32_t bar0 = base + sm.bars;
@@ -495,12 +536,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
     auto v_full = [&](int s) { return bar0 + 8 * (2 * sm.ks + s); };
     auto v_empty = [&](int s) { return bar0 + 8 * (2 * sm.ks + sm.vs + s); };
     const uint32_t bar1 = bar0 + 8 * (2 * sm.ks + 2 * sm.vs);
-    auto s_full = [&](int n) { return bar1 + 8 * place(n, sm.s_log2); };
-    auto s_free = [&](int n) { return bar1 + 8 * (kMaxBufs + place(n, sm.s_log2)); };
-    auto p_full = [&](int n) { return bar1 + 8 * (2 * kMaxBufs + place(n, sm.p_log2)); };
-    auto pv_done = [&](int n) { return bar1 + 8 * (3 * kMaxBufs + place(n, sm.p_log2)); };
-    auto sc_full = [&](int n) { return bar1 + 8 * (4 * kMaxBufs + place(n, sm.s_log2)); };     // the tile's scales are there
-    const uint32_t bar2 = bar1 + 8 * 5 * kMaxBufs;
+    auto s_full = [&](int n) { return bar1 + 8 * place(n, sm.s_log2); };       // the product, and the tile's scales
+    auto p_full = [&](int n) { return bar1 + 8 * (kMaxBufs + place(n, sm.p_log2)); };      // P^T there, S^T read
+    auto pv_done = [&](int n) { return bar1 + 8 * (2 * kMaxBufs + place(n, sm.p_log2)); };
+    const uint32_t bar2 = bar1 + 8 * 3 * kMaxBufs;
     auto vt_full = [&](int s) { return bar2 + 8 * s; };
     auto vt_free = [&](int s) { return bar2 + 8 * (kVBufs + s); };
     const uint32_t q_full = bar2 + 8 * 2 * kVBufs, o_free = q_full + 8, drain_qk = q_full + 16, drain_pv = q_full + 24;
@@ -513,9 +552,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
             const int j = i - 2 * (sm.ks + sm.vs);
             uint32_t count = 1;
             if (j < 0) count = i >= 2 * sm.ks + sm.vs ? D / 32 : 1;                             // v_empty: the converting warps
-            else if (j >= kMaxBufs && j < 3 * kMaxBufs) count = kShare;                         // s_free, p_full: one thread of a group
-            else if (j >= 5 * kMaxBufs && j < 5 * kMaxBufs + kVBufs) count = D / 32;            // vt_full
-            else if (j == 5 * kMaxBufs + 2 * kVBufs || j == 5 * kMaxBufs + 2 * kVBufs + 1) count = 4 * kGroups;     // q_full, o_free
+            else if (j < kMaxBufs) count = 2;                                                   // s_full: the products, the scales
+            else if (j < 2 * kMaxBufs) count = kShare;                                          // p_full: one thread of a group
+            else if (j >= 3 * kMaxBufs && j < 3 * kMaxBufs + kVBufs) count = D / 32;            // vt_full
+            else if (j == 3 * kMaxBufs + 2 * kVBufs || j == 3 * kMaxBufs + 2 * kVBufs + 1) count = 4 * kGroups;     // q_full, o_free
             mbar_init(bar0 + 8 * i, count);
         }
         if (lane == 0) *abort_flag = 0;
@@ -529,10 +569,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
             tmem_alloc(base + sm.misc, (uint32_t)P.tmem_cols);
             tmem_relinquish();
         }
-        // one chunk of columns, and the product takes two: the second stays zero
-        if (kC == 1 && warp >= kSoftmaxWarp0) {
+        // an odd number of chunks, and the product takes an even one: the last stays zero
+        if (8 * kC * kShare < NP && warp >= kSoftmaxWarp0) {
             for (int i = tid - 32 * kSoftmaxWarp0; i < 128 << sm.p_log2; i += kSoftmaxThreads)
-                *reinterpret_cast<uint4 *>(gbase + sm.p + (i >> 7) * (NP * 256) + 2048 + (i & 127) * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(gbase + sm.p + (i >> 7) * (NP * 256) + kC * kShare * 2048 + (i & 127) * 16) = make_uint4(0, 0, 0, 0);
             fence_proxy_async_smem();
         }
         grid_dependency_wait();
@@ -546,12 +586,9 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
     Walk walk(line, p.B, blockIdx.x);
     Segment seg;
 
-    // Registers go from the warps that issue and convert to those of the softmax, which keep their sums in them:
-    // 4 x 32 x 40 + 8 x 32 x 48 + 16 x 32 x 88 = 62464 of the launch's 28 x 32 x 72 = 64512.
-    static_assert(32 * (4 * 40 + 4 * kVBufs * 48 + 4 * kGroups * 88) <= kThreads * 72 && kThreads * 72 <= 65536, "register pool");
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer
-        fewer_registers<40>();
+        fewer_registers<kIssueRegs>();
         const uint64_t policy = l2_evict_first_policy();
         Ring kr, vr;
         const int boxes = p.page_size < kTilePos ? kTilePos / p.page_size : 1;
@@ -603,7 +640,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ K.Q^T issuer
-        fewer_registers<40>();
+        fewer_registers<kIssueRegs>();
         const uint32_t idesc = make_idesc_e4m3(128, NP, 0, 0);
         const uint32_t swz = D == 128 ? kSwizzle128B : kSwizzle64B;
         const uint64_t kd0 = make_smem_desc(base + sm.k, 16, 8 * D, swz), qd0 = make_smem_desc(base + sm.q, 16, 8 * D, swz);
@@ -616,7 +653,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
             qr.next(1);
             for (int j = 0; ok && j < seg.T; ++j, ++n) {
                 ok = wait(k_full(kr.idx), kr.parity, abort_flag);
-                if (n >> sm.s_log2) ok = wait(s_free(n), round_of(n, sm.s_log2) ^ 1u, abort_flag) && ok;
+                // S^T's buffer has been read, and (so that the softmax need not ask) the tile's P^T buffer
+                const int s_before = n - (1 << sm.s_log2);
+                if (s_before >= 0) ok = wait(p_full(s_before), round_of(s_before, sm.p_log2), abort_flag) && ok;
+                if (n >> sm.p_log2) ok = wait(pv_done(n), round_of(n, sm.p_log2) ^ 1u, abort_flag) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -644,7 +684,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         __syncwarp();
     } else if (warp == 2) {
         // ------------------------------------------------------------ P.V issuer
-        fewer_registers<40>();
+        fewer_registers<kIssueRegs>();
         const uint32_t idesc = make_idesc_f16(128, NP, 1);
         const uint64_t pd0 = make_smem_desc(base + sm.p, 128, 2048, kSwizzleNone);
         Ring vr, orr;
@@ -655,7 +695,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 ok = wait(o_free, orr.parity, abort_flag);     // the accumulators of the segment before have been read
                 orr.next(1);
             }
-            for (int j = 0; ok && j < seg.T; ++j, ++n) {
+            for (int j = 0, stream = 0; ok && j < seg.T; ++j, ++n) {
                 ok = wait(vt_full(vr.idx), vr.parity, abort_flag) && ok;
                 ok = wait(p_full(n), round_of(n, sm.p_log2), abort_flag) && ok;
                 ok = __all_sync(0xffffffffu, ok);
@@ -663,7 +703,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 tc_fence_after();
                 if (elect_one()) {
                     const uint64_t pd = pd0 + (uint64_t)(place(n, sm.p_log2) * (NP * 256 >> 4));
-                    const uint32_t d = tm_o + (j & (kStreams - 1)) * NP;
+                    const uint32_t d = tm_o + stream * NP;
 #pragma unroll
                     for (int c = 0; c < 8; ++c)
                         mma_f16_ts(d, tm_v + vr.idx * 64 + c * 8, pd + (uint64_t)(c * 16), idesc, j >= kStreams || c > 0);
@@ -672,6 +712,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 }
                 __syncwarp();
                 vr.next(kVBufs);
+                if (++stream == kStreams) stream = 0;
             }
         }
         if (elect_one()) {
@@ -681,7 +722,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         __syncwarp();
     } else if (warp >= kConvertWarp0 && warp < kSoftmaxWarp0) {
         // ------------------------------------------------- V codes to fp16 in tensor memory
-        fewer_registers<48>();
+        fewer_registers<kConvertRegs>();
         const int wq = warp & 3;                       // channels 32 wq .. + 31 = TMEM lanes
         const int set = (warp - kConvertWarp0) >> 2;   // tiles set, set + kVBufs, ... into V^T buffer `set`
         Ring vr;
@@ -739,7 +780,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         }
     } else if (warp == 3) {
         // ------------------------------------------------- the blocks' scales, from global to shared memory
-        fewer_registers<40>();
+        fewer_registers<kIssueRegs>();
         // lanes 0..7 the K scales of a tile's blocks, 16..23 the V scales
         const int blk = lane & 15, in_tile = blk << p.block_log2;
         const float *from = lane < 16 ? p.k_scale : p.v_scale;
@@ -756,12 +797,13 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
 #pragma unroll 1
             for (int j = -3; ok && j < seg.T; ++j) {
                 if (j >= 0) {
-                    if (n >> sm.s_log2) ok = wait(s_free(n), round_of(n, sm.s_log2) ^ 1u, abort_flag);
+                    const int before = n - (1 << sm.s_log2);
+                    if (before >= 0) ok = wait(p_full(before), round_of(before, sm.p_log2), abort_flag);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     if (blk < 8) scale_s[place(n, sm.s_log2) * 16 + (lane >> 4) * 8 + blk] = v0;
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(sc_full(n));
+                    if (lane == 0) mbar_arrive(s_full(n));
                     ++n;
                 }
                 v0 = v1;
@@ -775,24 +817,41 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         }
     } else if (warp >= kSoftmaxWarp0) {
         // ------------------------------------------------------------ softmax
-        more_registers<88>();
+        more_registers<softmax_regs(kGroups)>();
         const int grp = (warp - kSoftmaxWarp0) >> 2, bar_id = 1 + grp;
         constexpr int kAll = 1 + kGroups;                       // barrier of all softmax threads
+        constexpr int kBlock = block_of(kGroups, kC);
         const int stream = grp / kShare, part = grp % kShare;
         const int wq = warp & 3, row = wq * 32 + lane;          // TMEM lane: position of the tile, channel of the output
         const int stid = tid - 32 * kSoftmaxWarp0, gtid = stid & 127;
         const uint32_t lane_addr = (uint32_t)(wq * 32) << 16;
         // this group's chunks of columns
         const int c_lo = part * kC, col0 = c_lo * 8;
-        constexpr int kEach = kHalf ? 4 : 8;                    // sums a thread keeps of a chunk
         float *nm = nm_s + stream * NP + col0, *fac = fac_s + stream * NP + col0;
         float *tmx = reinterpret_cast<float *>(gbase + sm.tmx) + stream * 4 * NP + col0;
         float *my_sums = sums_s + (stream * 8 + wq) * NP + col0;            // + 4 NP: inside the span
         int n0 = 0;                                             // tiles of the segments before
         // No wait ends a loop here: a warp that left would leave its group at a barrier.  After a wait has run out all
         // others end at once, and what is computed then is void.
-        while (next_segment(line, walk, seg)) {
-            const int L = seg.len;
+        while (true) {
+            // one thread steps, the others read: what a segment is about is looked up again when it ends, not kept
+            if (stid == 0) {
+                if (!next_segment(line, walk, seg)) seg.T = 0;
+                seg_s.b = seg.b;
+                seg_s.head = seg.head;
+                seg_s.t0 = seg.t0;
+                seg_s.T = seg.T;
+                seg_s.len = seg.len;
+                seg_s.first = seg.first;
+                seg_s.last = seg.last;
+            }
+            named_sync(kAll, kSoftmaxThreads);
+            seg.T = seg_s.T;
+            if (seg.T == 0) break;
+            seg.b = seg_s.b;
+            seg.head = seg_s.head;
+            seg.t0 = seg_s.t0;
+            const int L = seg_s.len;
             const int vis0 = p.span[2 * seg.b], vis1 = p.span[2 * seg.b + 1];
 
             // ---- q as two E4M3 operand tiles
@@ -851,9 +910,9 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 if (lane == 0) mbar_arrive(q_full);
             }
 
-            float l[kC * kEach];
+            float l[kC * 8];
 #pragma unroll
-            for (int k = 0; k < kC * kEach; ++k) l[k] = 0.f;
+            for (int k = 0; k < kC * 8; ++k) l[k] = 0.f;
             for (int c = lane; c < kC * 8; c += 32) my_sums[c] = my_sums[4 * NP + c] = 0.f;
             bool l_in = false;                          // l holds sums of positions inside the span
             int k0 = 0;                                 // V scales are taken relative to 2^k0
@@ -876,9 +935,9 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 if (__builtin_expect(inside != l_in || j >= seg.T, 0)) {
 #pragma unroll
                     for (int c = 0; c < kC; ++c)
-                        add_to_sums(c, warp_sums<kEach>(l + c * kEach, lane), true, l_in);
+                        add_to_sums(c, warp_sums(l + c * 8, lane), true, l_in);
 #pragma unroll
-                    for (int k = 0; k < kC * kEach; ++k) l[k] = 0.f;
+                    for (int k = 0; k < kC * 8; ++k) l[k] = 0.f;
                     __syncwarp();
                     l_in = inside;
                     if (j >= seg.T) break;
@@ -888,14 +947,12 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 const bool begins = j == j_first;
                 const uint32_t s_addr = tm_s + place(n, sm.s_log2) * NP + lane_addr + col0;
 
-                wait(sc_full(n), round_of(n, sm.s_log2), abort_flag);
-                const float *sc = scale_s + place(n, sm.s_log2) * 16 + (row >> p.block_log2);
-                const float ck = scale * sc[0], vs = sc[8];
-                const int ve = (int)((__float_as_uint(vs) >> 23) & 0xFFu) - 127;
-                if (n >> sm.p_log2) wait(pv_done(n), round_of(n, sm.p_log2) ^ 1u, abort_flag);
                 wait(s_full(n), round_of(n, sm.s_log2), abort_flag);
                 __syncwarp();
                 tc_fence_after();
+                const float *sc = scale_s + place(n, sm.s_log2) * 16 + (row >> p.block_log2);
+                const float ck = scale * sc[0], vs = sc[8];
+                const int ve = (int)((__float_as_uint(vs) >> 23) & 0xFFu) - 127;
                 if (__builtin_expect(begins, 0)) {
                     // the first position's scores set the references, its block's V scale the scales'
                     if (wq == 0) {
@@ -926,10 +983,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                     const float vsr = vs * inv_k0, sign = back ? -1.f : 1.f;
                     if (__builtin_expect(!tail, 1)) {
                         const Seen all = {0, 0xFFFFFFFFu};
-                        top = softmax_pass<kC, kHalf, false>(s_addr, nm, ck, vsr, all, col0, prow, lane, sign, l);
+                        top = softmax_pass<kC, kBlock, false>(s_addr, nm, ck, vsr, all, col0, prow, sign, l);
                     } else {
                         const Seen seen = seen_by(pos - (L - gamma), G, gamma, p.branch_len);
-                        top = softmax_pass<kC, kHalf, true>(s_addr, nm, ck, vsr, seen, col0, prow, lane, sign, l);
+                        top = softmax_pass<kC, kBlock, true>(s_addr, nm, ck, vsr, seen, col0, prow, sign, l);
                     }
                     if (!back) {
                         // (all of the group's P^T is on its way to the tensor core when the vote is over)
@@ -973,10 +1030,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
 #pragma unroll
                     for (int c = 0; c < kC; ++c)
 #pragma unroll
-                            for (int k = 0; k < kEach; ++k) {
+                            for (int k = 0; k < 8; ++k) {
                                 // (NaN: the tile had brought an infinity, against which what was there before does not count)
-                                const float y = l[c * kEach + k];
-                                l[c * kEach + k] = y == y ? y * fac[c * 8 + (kHalf ? (lane >> 4) * 4 : 0) + k] : 0.f;
+                                const float y = l[c * 8 + k];
+                                l[c * 8 + k] = y == y ? y * fac[c * 8 + k] : 0.f;
                             }
                     if (!begins) {
                         // (the products of the stream's last tile have ended; the next are those of this one)
@@ -1016,15 +1073,12 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                         scores8<true>(r, nm + c * 8, ck, seen, col0 + c * 8, x);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) x[k] = in ? ex2(x[k]) : 0.f;
-                        add_to_sums(c, warp_sums<8>(x, lane), false, true);
+                        add_to_sums(c, warp_sums(x, lane), false, true);
                     }
                     tc_fence_before();
                     named_sync(bar_id, 128);            // (S^T has been read once more)
                 }
-                if (gtid == 0) {
-                    mbar_arrive(p_full(n));
-                    mbar_arrive(s_free(n));
-                }
+                if (gtid == 0) mbar_arrive(p_full(n));
                 last = n;
             }
             n0 += seg.T;
@@ -1035,8 +1089,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
             named_sync(kAll, kSoftmaxThreads);             // all sums are there
 
             // ---- a row's weights: each stream's part of the sum, in fac_s
-            const bool whole = seg.first && seg.last;
-            const int slot = part_slot(blockIdx.x, seg.first);
+            seg.b = seg_s.b;
+            seg.head = seg_s.head;
+            const bool whole = seg_s.first && seg_s.last;
+            const int slot = part_slot(blockIdx.x, seg_s.first);
             float *part_o = p.part_o + (size_t)slot * M * D;
             if (stid < M) {
                 const int col = stid;
@@ -1210,14 +1266,14 @@ bool make_pool_map(CUtensorMap *map, const uint8_t *pool, const PagedFp8Params &
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kStreams, int kC, bool kHalf>
+template <int kStreams, int kGroups, int kC>
 cudaError_t launch_attention(const KernelParams &P, const CUtensorMap &tk, const CUtensorMap &tv, cudaStream_t stream, int *launches)
 {
+    const auto kernel = attn_paged_fp8_kernel<kStreams, kGroups, kC>;
     const size_t smem = P.sm.total + 1024;
-    cudaError_t e = cudaFuncSetAttribute(attn_paged_fp8_kernel<kStreams, kC, kHalf>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_after(attn_paged_fp8_kernel<kStreams, kC, kHalf>, dim3((unsigned)P.a.n_cta), kThreads, smem, P.a.pdl != 0, stream,
-                        launches, P, tk, tv);
+    return launch_after(kernel, dim3((unsigned)P.a.n_cta), threads_of(kGroups), smem, P.a.pdl != 0, stream, launches, P, tk, tv);
 }
 
 }  // namespace
@@ -1229,10 +1285,11 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
 {
     KernelParams P;
     P.a = p;
-    P.NP = p.M > 96 ? 128 : (p.M + 15) & ~15;
+    const int n8 = p.M > 96 ? (p.M + 15) / 16 * 2 : (p.M + 7) / 8;      // chunks of eight columns
+    P.NP = (n8 + 1) / 2 * 16;
     // as many streams as tensor memory holds accumulators for, beside 2 x 64 columns of V^T and the S^T buffers
-    const int streams = P.NP <= 32 ? 4 : P.NP <= 96 ? 2 : 1;
-    const int s_log2 = kVBufs * 64 + (streams + 4) * P.NP <= 512 ? 2 : 1, p_log2 = P.NP <= 64 ? 2 : 1;
+    const int streams = P.NP <= 32 ? 4 : P.NP <= 48 ? 3 : P.NP <= 96 ? 2 : 1;
+    const int s_log2 = kVBufs * 64 + (streams + 4) * P.NP <= 512 ? 2 : 1, p_log2 = P.NP <= 96 ? 2 : 1;
     int cols = 32;
     while (cols < kVBufs * 64 + (streams + (1 << s_log2)) * P.NP) cols *= 2;
     P.tmem_cols = cols;
@@ -1244,15 +1301,21 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
     CUtensorMap tk, tv;
     if (!make_pool_map(&tk, k_pool, p) || !make_pool_map(&tv, v_pool, p)) return cudaErrorInvalidValue;
     cudaError_t e;
-    switch (P.NP / 16) {
-        case 1: e = p.M <= 8 ? launch_attention<4, 1, false>(P, tk, tv, stream, launches)
-                             : launch_attention<4, 2, false>(P, tk, tv, stream, launches); break;
-        case 2: e = launch_attention<4, 4, false>(P, tk, tv, stream, launches); break;
-        case 3: e = launch_attention<2, 3, false>(P, tk, tv, stream, launches); break;
-        case 4: e = launch_attention<2, 4, false>(P, tk, tv, stream, launches); break;
-        case 5: e = launch_attention<2, 5, false>(P, tk, tv, stream, launches); break;
-        case 6: e = launch_attention<2, 6, true>(P, tk, tv, stream, launches); break;
-        default: e = launch_attention<1, 4, false>(P, tk, tv, stream, launches); break;
+    switch (n8) {
+        case 1: e = launch_attention<4, 4, 1>(P, tk, tv, stream, launches); break;
+        case 2: e = launch_attention<4, 4, 2>(P, tk, tv, stream, launches); break;
+        case 3: e = launch_attention<4, 4, 3>(P, tk, tv, stream, launches); break;
+        case 4: e = launch_attention<4, 4, 4>(P, tk, tv, stream, launches); break;
+        case 5: e = launch_attention<3, 3, 5>(P, tk, tv, stream, launches); break;
+        case 6: e = launch_attention<3, 3, 6>(P, tk, tv, stream, launches); break;
+        case 7: e = launch_attention<2, 2, 7>(P, tk, tv, stream, launches); break;
+        case 8: e = launch_attention<2, 2, 8>(P, tk, tv, stream, launches); break;
+        case 9: e = launch_attention<2, 2, 9>(P, tk, tv, stream, launches); break;
+        case 10: e = launch_attention<2, 2, 10>(P, tk, tv, stream, launches); break;
+        case 11: e = launch_attention<2, 2, 11>(P, tk, tv, stream, launches); break;
+        case 12: e = launch_attention<2, 2, 12>(P, tk, tv, stream, launches); break;
+        case 14: e = launch_attention<1, 2, 7>(P, tk, tv, stream, launches); break;
+        default: e = launch_attention<1, 2, 8>(P, tk, tv, stream, launches); break;
     }
     if (e != cudaSuccess) return e;
     const int rows = p.B * p.gamma * p.Hq;
