@@ -598,6 +598,44 @@ lvspec_status_t lvspec_loose_accept_host(lvspec_ctx_t *ctx, int32_t batch, int32
                                          const lvspec_thresholds_t *thresholds,
                                          int32_t shift_window, int32_t *accept_len);
 
+/* ---- sampling ---------------------------------------------------------------
+ *
+ * The rule above compares draft tokens with the target's argmax (the paper samples nothing); a
+ * loop that samples its tokens (a correction or bonus token, a draft model's proposals, plain
+ * decoding) draws them here.  Per row of logits l, from the uniform number u that the caller gives:
+ *
+ *   T <= 0 (or NaN)  the argmax: lowest index among equals, NaN ranks as -inf (and raises
+ *                    LVSPEC_DEV_NAN_LOGIT); a row with nothing above -inf gives token 0.  Probability 1.
+ *   otherwise        w_i = exp((l_i - max l) / T).  Tokens are ordered by falling logit, equal ones by
+ *                    rising index, and each filter keeps a prefix of that order:
+ *     top_k          the first top_k tokens (<= 0 or >= vocab: all)
+ *     top_p          of those, the shortest prefix whose weights sum to at least top_p times theirs
+ *                    (>= 1 or NaN: all; at least the first token)
+ *     min_p          l_i >= max l + T ln(min_p), i.e. w_i >= min_p (<= 0 or NaN: all; above 1 counts as 1)
+ *                    What the shortest of the prefixes keeps has the sum W.
+ *   token            the first in index order at which the running sum of the kept weights exceeds u W
+ *   probability      w_token / W
+ *
+ * u below 0 or NaN counts as 0, 1 and above as the largest number below 1.  Weights are rounded to
+ * 2^-40 of the largest and summed as integers: a row gives the same token whatever rows are beside it.
+ *
+ *   logits       device, fp32 or bf16 (dtype)  rows of vocab, row_stride elements apart (>= vocab)
+ *   temperature, top_p, min_p  device, fp32 [rows]   NULL: 1, 1, 0
+ *   top_k        device, int32 [rows]                NULL: 0
+ *   uniform      device, fp32 [rows]
+ *   tokens       device, int32 [rows]   (written)
+ *   probs        device, fp32 [rows]    (written) may be NULL
+ *
+ * Needs no scratch memory.  rows = 0 does nothing.
+ * Errors: INVALID_ARG (null or misaligned pointers: logits to their element, the rest to 4 bytes;
+ * sizes or strides out of range, unknown dtype); UNSUPPORTED (vocab beyond LVSPEC_MAX_SAMPLE_VOCAB); CUDA. */
+#define LVSPEC_DTYPE_F32  0
+#define LVSPEC_DTYPE_BF16 1
+#define LVSPEC_MAX_SAMPLE_VOCAB 400000
+lvspec_status_t lvspec_sample(lvspec_ctx_t *ctx, int32_t rows, int32_t vocab, int32_t dtype, const void *logits,
+                              int64_t row_stride, const float *temperature, const int32_t *top_k, const float *top_p,
+                              const float *min_p, const float *uniform, int32_t *tokens, float *probs);
+
 /* ---- the paper's own relevance score -------------------------------------------
  *
  * Sec. 3.1, Eq. 4: the visual relevance A_s of draft token k is the mean of the

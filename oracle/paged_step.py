@@ -128,3 +128,42 @@ def attention(q, k_pool, v_pool, k_scale, v_scale, table, kv_len, span, block, b
                     out[b, g, hq] = p @ (np.abs(v[sees]) if absolute else v[sees])
                     mass[b, g, hq] = p[inside[sees]].sum()
     return out, mass
+
+
+def kept_tokens(logits, T, top_k, top_p, min_p):
+    """(tokens in falling order that the filters keep, all weights in fp64) of one row; T > 0."""
+    l = np.where(np.isnan(logits), -np.inf, np.asarray(logits, np.float64))
+    order = sorted(range(len(l)), key=lambda i: (-l[i], i))
+    top = l[order[0]]
+    with np.errstate(invalid="ignore", over="ignore"):
+        w = np.where(l == top, 1.0, np.exp((l - top) / T))
+    w = np.where(l == -np.inf, 0.0, w) if top > -np.inf else w
+    kept = order[:top_k] if 0 < top_k < len(l) else order
+    if top_p < 1:
+        share, total, n = 0.0, math.fsum(w[i] for i in kept), 0
+        for i in kept:
+            if n and share >= max(top_p, 0.0) * total:
+                break
+            share += w[i]
+            n += 1
+        kept = kept[:n]
+    if min_p > 0:
+        limit = top + T * math.log(min(min_p, 1.0))
+        kept = [i for i in kept if l[i] >= limit]
+    return kept, w
+
+
+def sample(logits, T, top_k, top_p, min_p, u):
+    """(token, probability, how far u is from the nearest border of the token's interval)."""
+    l = np.where(np.isnan(logits), -np.inf, np.asarray(logits, np.float64))
+    if not T > 0 or not l.max() > -np.inf:
+        return (int(l.argmax()) if l.max() > -np.inf else 0), 1.0, 1.0
+    kept, w = kept_tokens(logits, T, top_k, top_p, min_p)
+    u = min(max(u, 0.0), 1 - 2.0 ** -24) if u == u else 0.0
+    total = math.fsum(w[i] for i in kept)
+    run = 0.0
+    for i in sorted(kept):
+        if w[i] > 0 and run + w[i] > u * total:
+            return i, w[i] / total, min(u - run / total if run else 1.0, (run + w[i]) / total - u if run + w[i] < total else 1.0)
+        run += w[i]
+    raise AssertionError

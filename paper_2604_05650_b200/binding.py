@@ -38,6 +38,7 @@ EXPORTS = (
     "lvspec_verify_attention_fp8", "lvspec_verify_attention_strided", "lvspec_merge_polls",
     "lvspec_set_gpu_shared", "lvspec_merge_handed_over", "lvspec_plan_pages", "lvspec_append_paged_fp8",
     "lvspec_verify_attention_paged_fp8", "lvspec_attention_paged_fp8_workspace_bytes",
+    "lvspec_sample",
 )
 
 
@@ -137,6 +138,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.lvspec_verify_attention_paged_fp8.argtypes = [vp, S, PF, i32, i32] + [vp] * 10
     lib.lvspec_attention_paged_fp8_workspace_bytes.argtypes = [vp, S]
     lib.lvspec_attention_paged_fp8_workspace_bytes.restype = sz
+    lib.lvspec_sample.argtypes = [vp, i32, i32, i32, vp, i64] + [vp] * 7
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is ctypes.c_int and name not in ("lvspec_attention_splits", "lvspec_attention_splits_fp8"):
@@ -352,6 +354,14 @@ class Context:
             self._h, ctypes.byref(shape), ctypes.byref(cache), int(n_branches),
             shape.kv_capacity if max_kv_len is None else int(max_kv_len), _addr(q), _addr(k_pool), _addr(v_pool), _addr(k_scale),
             _addr(v_scale), _addr(block_table), _addr(kv_len), _addr(visual_span), _addr(out), _addr(visual_mass)))
+
+    def sample(self, rows, vocab, logits, temperature, top_k, top_p, min_p, uniform, tokens, probs=None, bf16=False,
+               row_stride=None) -> None:
+        """A token per row of logits (device fp32, or bf16); temperature, top_p, min_p (fp32 [rows]) and top_k (int32
+        [rows]) may be None; row_stride in elements (default: vocab)."""
+        self._check(self._lib.lvspec_sample(
+            self._h, int(rows), int(vocab), int(bool(bf16)), _addr(logits), int(vocab if row_stride is None else row_stride),
+            _addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p), _addr(uniform), _addr(tokens), _addr(probs)))
 
     def attention_paged_fp8_workspace_bytes(self, shape: AttnShape) -> int:
         return int(self._lib.lvspec_attention_paged_fp8_workspace_bytes(self._h, ctypes.byref(shape)))

@@ -1104,6 +1104,46 @@ lvspec_status_t lvspec_append_paged_fp8(lvspec_ctx_t *ctx, int32_t n_tokens, int
     return LVSPEC_OK;
 }
 
+lvspec_status_t lvspec_sample(lvspec_ctx_t *ctx, int32_t rows, int32_t vocab, int32_t dtype, const void *logits,
+                              int64_t row_stride, const float *temperature, const int32_t *top_k, const float *top_p,
+                              const float *min_p, const float *uniform, int32_t *tokens, float *probs)
+{
+    if (!ctx) return LVSPEC_ERR_INVALID_ARG;
+    if (rows < 0) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "rows < 0");
+    if (rows > 0 && (!logits || !uniform || !tokens)) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "null argument");
+    if (vocab < 1) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "vocab < 1");
+    if (dtype != LVSPEC_DTYPE_F32 && dtype != LVSPEC_DTYPE_BF16) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "unknown dtype");
+    if (row_stride < vocab || row_stride >= (int64_t(1) << 32))
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "row_stride outside vocab..2^32 - 1");
+    if ((reinterpret_cast<uintptr_t>(logits) & (dtype == LVSPEC_DTYPE_BF16 ? 1u : 3u)) || !aligned4(temperature) || !aligned4(top_k) ||
+        !aligned4(top_p) || !aligned4(min_p) || !aligned4(uniform) || !aligned4(tokens) || !aligned4(probs))
+        return fail(ctx, LVSPEC_ERR_INVALID_ARG, "misaligned device pointer");
+    if (vocab > LVSPEC_MAX_SAMPLE_VOCAB) return fail(ctx, LVSPEC_ERR_UNSUPPORTED, "vocab beyond LVSPEC_MAX_SAMPLE_VOCAB");
+    SampleParams p;
+    std::memset(&p, 0, sizeof p);
+    p.cluster = sample_cluster(vocab);
+    if ((int64_t)rows * p.cluster > 2147483647ll) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "rows out of range");
+    if (rows == 0) return LVSPEC_OK;
+    cudaError_t e = cudaSetDevice(ctx->device);
+    if (e != cudaSuccess) return cuda_fail(ctx, "cudaSetDevice", e);
+    p.logits = logits;
+    p.temperature = temperature;
+    p.top_k = top_k;
+    p.top_p = top_p;
+    p.min_p = min_p;
+    p.uniform = uniform;
+    p.tokens = tokens;
+    p.probs = probs;
+    p.status = ctx->status;
+    p.row_stride = row_stride;
+    p.vocab = vocab;
+    int launches = 0;
+    e = launch_sample(p, rows, dtype == LVSPEC_DTYPE_BF16, ctx->pdl, ctx->stream, &launches);
+    ctx->launches += launches;
+    if (e != cudaSuccess) return cuda_fail(ctx, "sampling kernel launch", e);
+    return LVSPEC_OK;
+}
+
 size_t lvspec_attention_paged_fp8_workspace_bytes(const lvspec_ctx_t *ctx, const lvspec_attn_shape_t *shape)
 {
     if (!ctx || !shape || shape->n_kv_heads < 1 || shape->gamma < 1 || shape->n_q_heads < shape->n_kv_heads || shape->head_dim < 1)

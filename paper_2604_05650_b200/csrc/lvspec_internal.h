@@ -238,6 +238,21 @@ struct PagedFp8Params {
     int32_t max_len, n_cta, pdl;
     float scale_log2;                   // log2(e) / sqrt(D)
 };
+// Sampling (sample.cu).
+struct SampleParams {
+    const void *logits;                 // [rows, vocab] fp32 or bf16, rows row_stride elements apart
+    const float *temperature, *top_p, *min_p, *uniform;      // [rows]; all but uniform optional
+    const int32_t *top_k;               // [rows], optional
+    int32_t *tokens;                    // [rows]
+    float *probs;                       // [rows], optional
+    uint32_t *status;
+    long long row_stride;
+    int32_t vocab, cluster;
+};
+int sample_cluster(int vocab);
+size_t sample_smem_bytes(int vocab, int cluster);
+cudaError_t launch_sample(const SampleParams &p, int rows, bool bf16, bool pdl, cudaStream_t stream, int *launches);
+
 size_t paged_fp8_scratch_bytes(int n_cta, int M, int D);
 cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool, const uint8_t *v_pool, cudaStream_t stream,
                                   int *launches);

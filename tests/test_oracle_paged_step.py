@@ -78,3 +78,19 @@ def test_a_query_that_sees_nothing_gives_zeros():
     out, mass = ref.attention(q, pool, pool, scale, scale, [[0], [0]], [2, 0], [[0, 1], [0, 0]], 16)
     assert (out[0, :2] == 0).all() and (out[0, 2:] == 1).all() and (out[1] == 0).all()
     assert mass[0, :, 0].tolist() == [0, 0, 1, 0.5]
+
+
+def test_sampling_by_hand():
+    l = np.log([0.1, 0.4, 0.2, 0.2, 0.1])
+    assert ref.kept_tokens(l, 1.0, 3, 1.0, 0.0)[0] == [1, 2, 3]
+    assert ref.kept_tokens(l, 1.0, 0, 0.55, 0.0)[0] == [1, 2]
+    assert ref.kept_tokens(l, 1.0, 2, 0.67, 0.0)[0] == [1, 2]              # 0.4 of 0.6 is below 0.67
+    assert ref.kept_tokens(l, 1.0, 2, 0.66, 0.0)[0] == [1]
+    assert ref.kept_tokens(l, 1.0, 0, 1.0, 0.45)[0] == [1, 2, 3]
+    assert ref.kept_tokens(l, 0.5, 0, 1.0, 0.3)[0] == [1]                  # the square of a half
+    assert ref.kept_tokens(l, 1.0, 0, 0.0, 0.0)[0] == [1]
+    assert [ref.sample(l, 1.0, 0, 1.0, 0.0, u)[0] for u in (0.0, 0.05, 0.15, 0.55, 0.75, 0.95)] == [0, 0, 1, 2, 3, 4]
+    assert ref.sample(l, 0.0, 0, 1.0, 0.0, 0.9)[:2] == (1, 1.0)
+    assert ref.sample([np.nan, -np.inf, np.nan], 1.0, 0, 1.0, 0.0, 0.9)[0] == 0
+    token, prob, _ = ref.sample(l, 1.0, 3, 1.0, 0.0, 0.6)
+    assert token == 2 and abs(prob - 0.25) < 1e-12
