@@ -1121,7 +1121,7 @@ lvspec_status_t lvspec_sample(lvspec_ctx_t *ctx, int32_t rows, int32_t vocab, in
     if (vocab > LVSPEC_MAX_SAMPLE_VOCAB) return fail(ctx, LVSPEC_ERR_UNSUPPORTED, "vocab beyond LVSPEC_MAX_SAMPLE_VOCAB");
     SampleParams p;
     std::memset(&p, 0, sizeof p);
-    p.cluster = sample_cluster(vocab);
+    p.cluster = sample_cluster(vocab, rows, ctx->n_sm);
     if ((int64_t)rows * p.cluster > 2147483647ll) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "rows out of range");
     if (rows == 0) return LVSPEC_OK;
     cudaError_t e = cudaSetDevice(ctx->device);

@@ -249,7 +249,7 @@ struct SampleParams {
     long long row_stride;
     int32_t vocab, cluster;
 };
-int sample_cluster(int vocab);
+int sample_cluster(int vocab, int rows, int n_sm);
 size_t sample_smem_bytes(int vocab, int cluster);
 cudaError_t launch_sample(const SampleParams &p, int rows, bool bf16, bool pdl, cudaStream_t stream, int *launches);
 

@@ -14,8 +14,10 @@
 // exchanges (a barrier each) and by the passes over shared memory, not by HBM.  A boundary is
 // found without sorting: a histogram over (M - l) in steps of T / 32, then the few hundred tokens of the bin that holds the
 // boundary are ranked by comparing all with all; a bin with more tokens than fit there (equal or nearly equal logits) is cut
-// into bins of the logits' bit patterns until it fits or holds a single value.  Top-p's bin is chosen by sums of weights
-// rounded to 2^-13, which is all 32-bit shared-memory atomics carry, and put right by exact sums.
+// into bins of the logits' bit patterns until it fits or holds a single value.  Top-p's bin is chosen by the bins' counts and
+// the weights of their middles, and put right by exact sums.
+#include <cfloat>
+
 #include "lvspec_internal.h"
 #include "sm100_ptx.cuh"
 
@@ -23,10 +25,9 @@ namespace lvspec {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 1024;
+constexpr int kBins = 2048;
 constexpr int kCandidates = 1024;       // tokens of a bin that are ranked directly
-constexpr int kMaxCluster = 8;
-constexpr int kCoarse = 13;             // bits of a weight in the histogram
+constexpr int kMaxCluster = 16;
 typedef unsigned long long u64;
 
 // ---- cluster -----------------------------------------------------------------------------
@@ -47,6 +48,12 @@ __device__ __forceinline__ uint32_t peer_address(uint32_t smem, uint32_t rank)
     return a;
 }
 __device__ __forceinline__ void st_peer(uint32_t a, u64 x) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(x) : "memory"); }
+__device__ __forceinline__ uint32_t add_peer(uint32_t a, uint32_t x)
+{
+    uint32_t old;
+    asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(a), "r"(x) : "memory");
+    return old;
+}
 __device__ __forceinline__ u64 ld_peer(uint32_t a)
 {
     u64 x;
@@ -63,7 +70,7 @@ __device__ __forceinline__ uint32_t key_of(float l)
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 
 struct Weight {
-    float top;              // the row's largest logit
+    float top;              // the row's largest logit, finite
     float per, per_rest;    // log2(e) / T in two parts
     __device__ __forceinline__ void set(float top_, float T)
     {
@@ -72,21 +79,20 @@ struct Weight {
         per = (float)c;
         per_rest = isinf(per) ? 0.f : (float)(c - (double)per);
     }
-    // round(2^40 exp((l - top) / T)): the difference and its product with `per` carried with their rounding errors, 2^x of
-    // the fraction good to 2^-22, its 24 bits shifted into place
+    // floor(2^40 exp((l - top) / T)): the difference and its product with `per` carried with their rounding errors, 2^x of the
+    // fraction good to 2^-22, its 24 bits shifted into place
     __device__ __forceinline__ u64 operator()(float l) const
     {
-        if (l == top) return 1ull << 40;        // (both infinite too)
         const float d = l - top, z = d - l;
         const float d_rest = (l - (d - z)) + (-top - z);
         const float y = d * per;
-        if (!(y > -42.f)) return 0;             // (also -inf, and a top that is infinite)
-        const float n = rintf(y);
+        const float t = y + 12582912.f, n = t - 12582912.f;         // 1.5 * 2^23: y to the nearest integer, in the low bits of t
         const float f = (y - n) + (fmaf(d, per, -y) + fmaf(d, per_rest, d_rest * per));
         const uint32_t e = __float_as_uint(ptx::ex2(f));
-        const int shift = (int)n + (int)(e >> 23) - 127 + 17;
-        const u64 m = (e & 0x7FFFFFu) | 0x800000u;
-        return shift >= 0 ? m << shift : (m + (1ull << (-shift - 1))) >> -shift;
+        const uint32_t m = (e & 0x7FFFFFu) | 0x800000u;
+        const int down = 127 - (int)(e >> 23) - (int)(__float_as_uint(t) - 0x4B400000u);        // m << 17 >> down
+        const u64 w = ((u64)m << 17) >> down;
+        return y > -42.f ? w : 0;
     }
 };
 
@@ -100,31 +106,45 @@ struct Place {
 struct Shared {
     u64 box[2][kMaxCluster][4];         // what the CTAs tell one another, two rounds by turns
     u64 warp_val[3][kWarps];
-    uint32_t count[kBins], mass[kBins];             // of this CTA's tokens
-    uint32_t all_count[kBins], all_mass[kBins];     // of the whole row's
-    u64 cand[kCandidates];              // key, index of a bin's tokens
-    u64 cum[2];
+    uint32_t bins[kBins], all_bins[kBins];      // a histogram of this CTA's tokens, of the whole row's
+    u64 cand[kCandidates], cand_weight[kCandidates];    // key and index of a bin's tokens; their weights
+    u64 cum;
     int bin, n_cand, answer;
     Place place;
 };
 
 struct Row {
     Shared &s;
-    const float *v;                     // this CTA's logits, v[0 .. n)
-    int n, first;                       // first: the index of v[0]
+    const float *v;                     // this CTA's logits, v[0 .. n); before and behind them, to 16-byte borders, -inf
+    int n, first, pad;                  // first: the index of v[0]; pad: logits from the first border to v[0]
     int n_cta, rank, turn;
     Weight weight;
     float bins_per;                     // 32 / T
 
     __device__ __forceinline__ Row(Shared &s_) : s(s_), turn(0) {}
 
-    // Sums (op 0), or largest values (op 1), of up to three numbers per thread over the row; every CTA's in box[slot].
+    // f(logit, its place in v) for this CTA's logits above -inf, four side by side
+    template <typename F>
+    __device__ __forceinline__ void for_each(F f) const
+    {
+        const float4 *g4 = reinterpret_cast<const float4 *>(v - pad);
+        for (int g = threadIdx.x; g * 4 < pad + n; g += kThreads) {
+            const float4 x = g4[g];
+            const float l[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (l[k] > -INFINITY) f(l[k], g * 4 + k - pad);
+        }
+    }
+
+    // Sums (op 0), or largest values (op 1), of kN numbers per thread over the row; every CTA's in box[slot].
+    template <int kN>
     __device__ int gather(u64 a, u64 b, u64 c, int op)
     {
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
         u64 x[3] = {a, b, c};
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = 0; k < kN; ++k) {
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) {
                 const u64 y = __shfl_xor_sync(0xffffffffu, x[k], o);
@@ -137,7 +157,7 @@ struct Row {
         ++turn;
         if (warp == 0) {
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
+            for (int k = 0; k < kN; ++k) {
                 u64 t = lane < kWarps ? s.warp_val[k][lane] : 0;
 #pragma unroll
                 for (int o = kWarps / 2; o > 0; o >>= 1) {
@@ -159,44 +179,46 @@ struct Row {
         }
         return t;
     }
+    // The nearest bin to (top - l) bins_per; it falls as l rises, whatever the rounding.
     __device__ __forceinline__ int bin_of(float l) const
     {
-        // (falls as l rises, whatever the rounding; infinities: bin 0 for the top, the last for -inf)
-        const float t = (weight.top - l) * bins_per;
-        return l == weight.top ? 0 : t < (float)(kBins - 1) ? (int)t : kBins - 1;
+        const float t = fminf((weight.top - l) * bins_per, (float)(kBins - 1));
+        return (int)(__float_as_uint(t + 12582912.f) - 0x4B400000u);          // (1.5 * 2^23: the integer is in the low bits)
     }
-    // Bins of the whole row from those of the CTAs: each CTA adds up its share and hands it to all.
+    // Weight of a logit in the middle of a bin (none for the last, which has no end)
+    __device__ __forceinline__ u64 bin_weight(int b) const { return b < kBins - 1 ? weight(weight.top - b / bins_per) : 0; }
+    // Bins of the whole row from those of the CTAs (which a cluster barrier has seen done): each CTA adds up its share and hands it
+    // to all.
     __device__ void share_bins()
     {
-        cluster_sync();
         const int per = kBins / n_cta;
         for (int i = threadIdx.x; i < per / 2; i += kThreads) {
             const int bin = rank * per + 2 * i;
-            u64 c = 0, m = 0;           // two 32-bit counters side by side: neither overflows
-            for (int r = 0; r < n_cta; ++r) {
-                c += ld_peer(peer_address(ptx::smem_u32(&s.count[bin]), r));
-                m += ld_peer(peer_address(ptx::smem_u32(&s.mass[bin]), r));
-            }
-            for (int r = 0; r < n_cta; ++r) {
-                st_peer(peer_address(ptx::smem_u32(&s.all_count[bin]), r), c);
-                st_peer(peer_address(ptx::smem_u32(&s.all_mass[bin]), r), m);
-            }
+            u64 c = 0;                  // two 32-bit counters side by side: neither overflows
+            for (int r = 0; r < n_cta; ++r) c += ld_peer(peer_address(ptx::smem_u32(&s.bins[bin]), r));
+            for (int r = 0; r < n_cta; ++r) st_peer(peer_address(ptx::smem_u32(&s.all_bins[bin]), r), c);
         }
         cluster_sync();
     }
     __device__ void clear_bins()
     {
-        for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = s.mass[i] = 0;
+        for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
         __syncthreads();
     }
-    // First bin at which the running sum of `a` reaches `want` (the last one if none does); the sum before it.
-    __device__ int bin_reaching(const uint32_t *a, u64 want, u64 &before)
+    // First bin at which the running sum, of tokens or (`each`: weight of a token of a bin) of weights, reaches `want`; kBins if none
+    // does.  The sum before it.
+    template <typename Each>
+    __device__ int bin_reaching(u64 want, u64 &before, Each each)
     {
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
         constexpr int kEach = kBins / kThreads;
-        u64 mine = 0;
+        u64 a[kEach], mine = 0;
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) mine += a[tid * kEach + k];
+        for (int k = 0; k < kEach; ++k) {
+            const uint32_t c = s.all_bins[tid * kEach + k];
+            a[k] = c ? c * each(tid * kEach + k) : 0;
+            mine += a[k];
+        }
         u64 in = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -208,84 +230,78 @@ struct Row {
         __syncthreads();
         u64 at = in - mine;
         for (int w = 0; w < warp; ++w) at += s.warp_val[0][w];
+#pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const u64 next = at + a[tid * kEach + k];
-            const bool last = tid * kEach + k == kBins - 1;
-            if (at < want && (next >= want || last)) {
+            if (at < want && at + a[k] >= want) {
                 s.bin = tid * kEach + k;
-                s.cum[0] = at;
+                s.cum = at;
             }
-            at = next;
+            at += a[k];
         }
         __syncthreads();
         const int bin = s.bin;
-        before = s.cum[0];
+        before = s.cum;
         __syncthreads();
         return bin;
     }
 
     // Puts a bin right by exact sums of the row's weights: the one in which the running sum over the bins reaches `need`.  `bin_at`
-    // says which bin of 0..kBins - 1 a token is in (-1: none).  `before`: the sum of the bins before it.
+    // says which bin of 0..kBins - 1 a logit is in (-1: none).  `before`: the sum of the bins before it; `count`: its tokens.
     template <typename BinAt>
-    __device__ int settle(int b, u64 need, u64 &before, BinAt bin_at)
+    __device__ int settle(int b, u64 need, u64 &before, u64 &count, BinAt bin_at)
     {
-        if (b >= kBins) b = 0;
+        if (b >= kBins) b = kBins - 1;
         int lo = 0, hi = kBins - 1;
         for (int turn_no = 0;; ++turn_no) {
-            u64 above = 0, inside = 0, below = 0;
-            for (int i = threadIdx.x; i < n; i += kThreads) {
-                const int bb = bin_at(i);
-                if (bb < 0) continue;
-                const u64 w = weight(v[i]);
+            u64 above = 0, inside = 0, tokens = 0;
+            for_each([&](float l, int) {
+                const int bb = bin_at(l);
+                if (bb < 0 || bb > b) return;
+                const u64 w = weight(l);
                 if (bb < b) above += w;
-                else if (bb == b) inside += w;
-                else below += w;
-            }
-            const int slot = gather(above, inside, below, 0);
-            const u64 a = of_all(slot, 0, 0), in = of_all(slot, 1, 0), rest = of_all(slot, 2, 0);
+                else {
+                    inside += w;
+                    ++tokens;
+                }
+            });
+            const int slot = gather<3>(above, inside, tokens, 0);
+            const u64 a = of_all(slot, 0, 0), in = of_all(slot, 1, 0);
             before = a;
+            count = of_all(slot, 2, 0);
             if (a >= need && b > lo) hi = b - 1;
-            else if (a + in < need && rest > 0 && b < hi) lo = b + 1;
+            else if (a + in < need && b < hi) lo = b + 1;
             else return b;
-            // (the bin chosen by coarse sums is off by one if at all; without such a choice the range is halved)
+            // (the bin chosen by the bins' middles is off by one if at all; otherwise the range is halved)
             b = turn_no < 2 ? (a >= need ? b - 1 : b + 1) : (lo + hi) / 2;
         }
     }
 
-    // The last token of the prefix: of the tokens of bin `bin` of (M - l), the one at which the count (by_mass = false) or the sum of
-    // weights reaches `need`, counted from the bin's first.
-    __device__ Place resolve(int bin, bool by_mass, u64 need)
+    // The last token of the prefix: of the `total` tokens of bin `bin` of (M - l), the one at which the count (by_mass = false) or
+    // the sum of weights reaches `need`, counted from the bin's first.
+    __device__ Place resolve(int bin, bool by_mass, u64 need, u64 total)
     {
         const int tid = threadIdx.x, lane = tid & 31;
         uint32_t lo = 0, hi = 0xFFFFFFFFu;              // keys of the bin
+        auto in_bin = [&](float l, uint32_t &k) {
+            k = key_of(l);
+            return bin_of(l) == bin && k >= lo && k <= hi;
+        };
         for (;;) {
-            // how many tokens, and between which keys
-            u64 most = 0, least = 0, count = 0;
-            for (int i = tid; i < n; i += kThreads) {
-                const uint32_t k = key_of(v[i]);
-                if (bin_of(v[i]) == bin && k >= lo && k <= hi) {
-                    most = max((u64)k, most);
-                    least = max((u64)(0xFFFFFFFFu - k), least);
-                    ++count;
-                }
-            }
-            int slot = gather(count, 0, 0, 0);
-            const u64 total = of_all(slot, 0, 0);
-            int before = 0;
-            for (int r = 0; r < rank; ++r) before += (int)s.box[slot][r][0];
             if (total <= kCandidates) {
-                // ---- rank them all
-                if (tid == 0) s.n_cand = before;
-                __syncthreads();
-                for (int i = tid; i < n; i += kThreads) {
-                    const uint32_t k = key_of(v[i]);
-                    if (bin_of(v[i]) == bin && k >= lo && k <= hi) {
-                        const int at = atomicAdd(&s.n_cand, 1);
-                        for (int r = 0; r < n_cta; ++r)
-                            st_peer(peer_address(ptx::smem_u32(&s.cand[at]), r), ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)(first + i)));
+                // ---- rank them all: places in the list are handed out by the first CTA
+                const uint32_t counter = peer_address(ptx::smem_u32(&s.n_cand), 0);
+                for_each([&](float l, int i) {
+                    uint32_t k;
+                    if (!in_bin(l, k)) return;
+                    const uint32_t at = add_peer(counter, 1u);
+                    const u64 w = by_mass ? weight(l) : 1;
+                    for (int r = 0; r < n_cta; ++r) {
+                        st_peer(peer_address(ptx::smem_u32(&s.cand[at]), r), ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)(first + i)));
+                        st_peer(peer_address(ptx::smem_u32(&s.cand_weight[at]), r), w);
                     }
-                }
+                });
                 cluster_sync();
+                if (tid == 0) s.n_cand = 0;
                 // larger words come first; lanes side by side share a candidate's comparisons
                 const int m = (int)total;
                 int side = 1;
@@ -295,17 +311,12 @@ struct Row {
                     const u64 mine = c < m ? s.cand[c] : 0;
                     u64 sum = 0;
                     if (c < m)
-                        for (int j = tid % side; j < m; j += side) {
-                            const u64 other = s.cand[j];
-                            if (other > mine) sum += by_mass ? weight(logit_of((uint32_t)(other >> 32))) : 1;
-                        }
+                        for (int j = tid % side; j < m; j += side)
+                            if (s.cand[j] > mine) sum += s.cand_weight[j];
                     for (int o = side / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    if (c < m && tid % side == 0) {
-                        const u64 own = by_mass ? weight(logit_of((uint32_t)(mine >> 32))) : 1;
-                        if (sum < need && sum + own >= need) {
-                            s.place.key = (uint32_t)(mine >> 32);
-                            s.place.index = (int)(0xFFFFFFFFu - (uint32_t)mine);
-                        }
+                    if (c < m && tid % side == 0 && sum < need && sum + s.cand_weight[c] >= need) {
+                        s.place.key = (uint32_t)(mine >> 32);
+                        s.place.index = (int)(0xFFFFFFFFu - (uint32_t)mine);
                     }
                 }
                 __syncthreads();
@@ -313,7 +324,15 @@ struct Row {
                 __syncthreads();
                 return p;
             }
-            slot = gather(most, least, 0, 1);
+            u64 most = 0, least = 0, count = 0;
+            for_each([&](float l, int) {
+                uint32_t k;
+                if (!in_bin(l, k)) return;
+                most = max((u64)k, most);
+                least = max((u64)(0xFFFFFFFFu - k), least);
+                ++count;
+            });
+            int slot = gather<2>(most, least, 0, 1);
             const uint32_t k_hi = (uint32_t)of_all(slot, 0, 1), k_lo = 0xFFFFFFFFu - (uint32_t)of_all(slot, 1, 1);
             if (k_hi == k_lo) {
                 // ---- one value: the place among equals is a matter of index
@@ -321,11 +340,13 @@ struct Row {
                 u64 nth = each ? (need + each - 1) / each : 1;              // counted from 1
                 if (nth > total) nth = total;
                 if (nth < 1) nth = 1;
-                // (`before` equals sit in the CTAs before this one)
-                const u64 here = count_sum(count);
+                slot = gather<1>(count, 0, 0, 0);
+                u64 before = 0;
+                for (int r = 0; r < rank; ++r) before += s.box[slot][r][0];
+                const u64 here = s.box[slot][rank][0];
                 if (tid == 0) s.answer = -1;
                 __syncthreads();
-                if (nth > (u64)before && nth <= (u64)before + here && tid < 32) {
+                if (nth > before && nth <= before + here && tid < 32) {
                     u64 left = nth - before;
                     for (int i0 = 0; i0 < n; i0 += 32) {
                         const bool is = i0 + lane < n && key_of(v[i0 + lane]) == k_hi;
@@ -339,50 +360,42 @@ struct Row {
                     }
                 }
                 __syncthreads();
-                slot = gather(tid == 0 ? (u64)(s.answer + 1) : 0, 0, 0, 1);
+                slot = gather<1>(tid == 0 ? (u64)(s.answer + 1) : 0, 0, 0, 1);
                 Place p;
                 p.key = k_hi;
                 p.index = (int)of_all(slot, 0, 1) - 1;
                 return p;
             }
-            // ---- bins of the keys; exact counts, and for weights a round of exact sums
+            // ---- bins of the keys
             int shift = 0;
             while (((k_hi - k_lo) >> shift) >= (uint32_t)kBins) ++shift;
+            lo = k_lo;
+            hi = k_hi;
+            auto key_bin = [&](float l) {
+                uint32_t k;
+                return in_bin(l, k) ? (int)((k_hi - k) >> shift) : -1;
+            };
             clear_bins();
-            for (int i = tid; i < n; i += kThreads) {
-                const uint32_t k = key_of(v[i]);
-                if (bin_of(v[i]) == bin && k >= k_lo && k <= k_hi) {
-                    const int b = (int)((k_hi - k) >> shift);
-                    atomicAdd(&s.count[b], 1u);
-                    if (by_mass) atomicAdd(&s.mass[b], (uint32_t)(weight(v[i]) >> (40 - kCoarse)));
-                }
-            }
+            for_each([&](float l, int) {
+                const int b = key_bin(l);
+                if (b >= 0) atomicAdd(&s.bins[b], 1u);
+            });
+            cluster_sync();
             share_bins();
             u64 at = 0;
-            int b = bin_reaching(by_mass ? s.all_mass : s.all_count, by_mass ? (need >> (40 - kCoarse)) + 1 : need, at);
-            if (by_mass)
-                b = settle(b, need, at, [&](int i) {
-                    const uint32_t k = key_of(v[i]);
-                    return bin_of(v[i]) == bin && k >= k_lo && k <= k_hi ? (int)((k_hi - k) >> shift) : -1;
-                });
+            int b;
+            if (by_mass) {
+                b = bin_reaching(need, at, [&](int k) { return weight(logit_of(k_hi - ((uint32_t)k << shift))); });
+                b = settle(b, need, at, total, key_bin);
+            } else {
+                b = bin_reaching(need, at, [](int) { return 1ull; });
+                total = s.all_bins[b];
+            }
             need -= at;
             const uint32_t top_key = k_hi - ((uint32_t)b << shift);
             hi = top_key;
             lo = max(k_lo, top_key - min(top_key, (1u << shift) - 1u));
         }
-    }
-    // this CTA's sum of a number per thread
-    __device__ u64 count_sum(u64 x)
-    {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-        if (lane == 0) s.warp_val[0][warp] = x;
-        __syncthreads();
-        u64 t = 0;
-        for (int w = 0; w < kWarps; ++w) t += s.warp_val[0][w];
-        __syncthreads();
-        return t;
     }
 };
 
@@ -401,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
     const float T = p.temperature ? p.temperature[row] : 1.f;
-    int top_k = p.top_k ? p.top_k[row] : 0;
+    const int top_k = p.top_k ? p.top_k[row] : 0;
     const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
     float u = p.uniform[row];
     u = u > 0.f ? fminf(u, 0.99999994f) : 0.f;
@@ -414,6 +427,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const char *from = static_cast<const char *>(p.logits) + ((size_t)row * p.row_stride + c0) * esz;
     const int pad = (int)((reinterpret_cast<uintptr_t>(from) & 15u) / esz);          // elements before the first 16-byte group's
     r.v = values + pad;
+    r.pad = pad;
     r.n = c1 - c0;
     r.first = c0;
     bool nan_seen = false;
@@ -433,36 +447,42 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         return x;
     };
     const int groups = (pad + r.n + kVec - 1) / kVec;
-    for (int g = tid; g < groups; g += kThreads) {
-        const int e = g * kVec - pad;                   // of the chunk
-        float x[kVec];
-        if (e >= 0 && e + kVec <= r.n) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(from + (long long)e * (long long)esz);
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+    constexpr int kAhead = 4;           // 16-byte loads of a thread in flight
+    for (int g0 = tid; g0 < groups; g0 += kAhead * kThreads) {
+        uint4 w[kAhead];
 #pragma unroll
-            for (int k = 0; k < kVec; ++k)
-                x[k] = kBf16 ? __uint_as_float(k & 1 ? ww[k / 2] & 0xFFFF0000u : ww[k / 2] << 16) : __uint_as_float(ww[k % 4]);
-        } else {
+        for (int a = 0; a < kAhead; ++a) {
+            const int e = (g0 + a * kThreads) * kVec - pad;         // place in the chunk
+            if (e >= 0 && e + kVec <= r.n) w[a] = *reinterpret_cast<const uint4 *>(from + (long long)e * (long long)esz);
+        }
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int g = g0 + a * kThreads, e = g * kVec - pad;
+            if (g >= groups) break;
+            const bool whole = e >= 0 && e + kVec <= r.n;
+            const uint32_t ww[4] = {w[a].x, w[a].y, w[a].z, w[a].w};
+            float x[kVec];
 #pragma unroll
             for (int k = 0; k < kVec; ++k) {
                 x[k] = -INFINITY;
-                if (e + k >= 0 && e + k < r.n)
+                if (whole)
+                    x[k] = kBf16 ? __uint_as_float(k & 1 ? ww[k / 2] & 0xFFFF0000u : ww[k / 2] << 16) : __uint_as_float(ww[k % 4]);
+                else if (e + k >= 0 && e + k < r.n)
                     x[k] = kBf16 ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(from)[e + k] << 16)
                                  : reinterpret_cast<const float *>(from)[e + k];
+                if (whole || (e + k >= 0 && e + k < r.n)) x[k] = take(x[k], c0 + e + k);
             }
+#pragma unroll
+            for (int k = 0; k < kVec; k += 4)
+                *reinterpret_cast<float4 *>(values + g * kVec + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
         }
-#pragma unroll
-        for (int k = 0; k < kVec; ++k)
-            if (e + k >= 0 && e + k < r.n) x[k] = take(x[k], c0 + e + k);
-#pragma unroll
-        for (int k = 0; k < kVec; k += 4)
-            *reinterpret_cast<float4 *>(values + g * kVec + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
     }
     if (nan_seen) atomicOr(p.status, LVSPEC_DEV_NAN_LOGIT);
+    if (tid == 0) s.n_cand = 0;
     r.clear_bins();
     // largest logit, at its lowest index
     const u64 first_best = best_i == 0x7fffffff ? 0 : ((u64)key_of(best) << 32) | (0xFFFFFFFFu - (uint32_t)best_i);
-    const u64 largest = r.of_all(r.gather(first_best, 0, 0, 1), 0, 1);
+    const u64 largest = r.of_all(r.gather<1>(first_best, 0, 0, 1), 0, 1);
     const float top = logit_of((uint32_t)(largest >> 32));
     const int top_i = (int)(0xFFFFFFFFu - (uint32_t)largest);
     if (!(T > 0.f) || !(top > -INFINITY)) {
@@ -473,66 +493,77 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         }
         return;
     }
-    r.weight.set(top, T);
-    // (a top that is infinite has all other tokens in the last bin; a temperature that is, all in the first)
-    r.bins_per = fminf(32.f / T, 3.0e38f);
+    r.weight.set(fminf(top, FLT_MAX), T);
+    if (top > FLT_MAX) {
+        // infinite logits: as the largest finite number they keep all the weight among them (unless that number is there too, or T
+        // so large that others count beside it)
+        for (int i = tid; i < r.n; i += kThreads)
+            if (values[pad + i] > FLT_MAX) values[pad + i] = FLT_MAX;
+        __syncthreads();
+    }
+    r.bins_per = fmaxf(fminf(32.f / T, 3.0e38f), 1.0e-37f);
 
     // ---- the shortest prefix that the filters keep
     Place place = {0u, 0x7fffffff};                     // everything
-    const bool by_k = top_k > 0 && top_k < p.vocab, by_p = top_p < 1.f;
+    bool by_k = top_k > 0 && top_k < p.vocab;
+    const bool by_p = top_p < 1.f;
+    u64 before = 0;
     if (by_k || by_p) {
-        u64 all = 0;
-        for (int i = tid; i < r.n; i += kThreads) {
-            const int b = r.bin_of(r.v[i]);
-            if (by_k) atomicAdd(&s.count[b], 1u);
-            if (by_p) {
-                const u64 w = r.weight(r.v[i]);
-                all += w;
-                const uint32_t m = (uint32_t)(w >> (40 - kCoarse));
-                if (m) atomicAdd(&s.mass[b], m);
-            }
-        }
+        // (the last bin has no end: most of a peaked row is there, and all at one counter would wait for one another)
+        u64 kept = 0;                   // weights
+        uint32_t in_last = 0;
+        r.for_each([&](float l, int) {
+            const int b = r.bin_of(l);
+            if (b < kBins - 1) atomicAdd(&s.bins[b], 1u);
+            else ++in_last;
+            if (by_p) kept += r.weight(l);
+        });
+        in_last = __reduce_add_sync(0xffffffffu, in_last);
+        if (lane == 0 && in_last) atomicAdd(&s.bins[kBins - 1], in_last);
+        u64 whole = r.of_all(r.gather<1>(kept, 0, 0, 0), 0, 0);
         r.share_bins();
-        u64 before = 0;
         if (by_k) {
-            const int b = r.bin_reaching(s.all_count, (u64)top_k, before);
-            place = r.resolve(b, false, (u64)top_k - before);
+            const int b = r.bin_reaching((u64)top_k, before, [](int) { return 1ull; });
+            by_k = b < kBins;           // (fewer logits above -inf than that: no filter)
+            if (by_k) place = r.resolve(b, false, (u64)top_k - before, s.all_bins[b]);
         }
         if (by_p) {
-            // what top-k leaves, of which top-p keeps a share
-            u64 kept = all;
+            // of the weight that top-k leaves top-p keeps a share
             if (by_k) {
                 kept = 0;
-                for (int i = tid; i < r.n; i += kThreads)
-                    if (place.reaches(key_of(r.v[i]), c0 + i)) kept += r.weight(r.v[i]);
+                r.for_each([&](float l, int i) {
+                    if (place.reaches(key_of(l), c0 + i)) kept += r.weight(l);
+                });
+                whole = r.of_all(r.gather<1>(kept, 0, 0, 0), 0, 0);
             }
-            const u64 whole = r.of_all(r.gather(kept, 0, 0, 0), 0, 0);
-            // the first sum that is not below p * whole; at least the first token
-            const double share = fmax((double)top_p, 0.0) * (double)whole;
-            u64 need = (u64)ceil(share);
-            if (need < 1) need = 1;
-            if (need > whole) need = whole;
-            // (top-k's boundary has been resolved through the same arrays: the coarse sums are still the row's unless it was cut
-            // into bins of keys, and any bin will do to begin with)
-            int b = r.bin_reaching(s.all_mass, (need >> (40 - kCoarse)) + 1, before);
-            b = r.settle(b, need, before, [&](int i) { return r.bin_of(r.v[i]); });
-            const Place q = r.resolve(b, true, need - before);
+            // the first sum that is not below top_p * whole; at least the first token
+            const u64 need = min(whole, max((u64)1, (u64)ceil(fmax((double)top_p, 0.0) * (double)whole)));
+            u64 total = 0;
+            int b = r.bin_reaching(need, before, [&](int k) { return r.bin_weight(k); });
+            b = r.settle(b, need, before, total, [&](float l) { return r.bin_of(l); });
+            const Place q = r.resolve(b, true, need - before, total);
             if (!by_k || q.key > place.key || (q.key == place.key && q.index < place.index)) place = q;
         }
     }
     uint32_t least_key = 0;
-    if (min_p > 0.f) least_key = key_of(__double2float_ru((double)top + (double)T * log(fmin((double)min_p, 1.0))) + 0.f);
+    if (min_p > 0.f) least_key = key_of(__double2float_ru((double)r.weight.top + (double)T * log(fmin((double)min_p, 1.0))) + 0.f);
 
-    // ---- running sums in index order: a lane's tokens are neighbours (an odd number of them: no two lanes on a bank)
-    const int each = ((r.n + kThreads - 1) / kThreads) | 1;
-    const int i0 = min(r.n, tid * each), i1 = min(r.n, i0 + each);
-    auto kept = [&](int i) -> u64 {
-        const uint32_t k = key_of(r.v[i]);
-        return k >= least_key && place.reaches(k, c0 + i) ? r.weight(r.v[i]) : 0;
+    // ---- running sums in index order: a thread's tokens are neighbours, an odd number of groups of four (no two threads of
+    // a quarter warp then meet on a bank)
+    const int each = ((groups * kVec / 4 + kThreads - 1) / kThreads) | 1;
+    const float4 *g4 = reinterpret_cast<const float4 *>(values);
+    const int g_end = min((tid + 1) * each, (pad + r.n + 3) / 4);
+    auto kept_weight = [&](float l, int i) -> u64 {
+        const uint32_t k = key_of(l);
+        return l > -INFINITY && k >= least_key && place.reaches(k, c0 + i) ? r.weight(l) : 0;
     };
     u64 mine = 0;
-    for (int i = i0; i < i1; ++i) mine += kept(i);
-    const int slot = r.gather(mine, 0, 0, 0);
+    for (int g = tid * each; g < g_end; ++g) {
+        const float4 x = g4[g];
+        const int i = g * 4 - pad;
+        mine += kept_weight(x.x, i) + kept_weight(x.y, i + 1) + kept_weight(x.z, i + 2) + kept_weight(x.w, i + 3);
+    }
+    const int slot = r.gather<1>(mine, 0, 0, 0);
     const u64 total = r.of_all(slot, 0, 0);
     u64 at = 0;
     for (int k = 0; k < r.rank; ++k) at += s.box[slot][k][0];
@@ -548,8 +579,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     for (int w = 0; w < warp; ++w) at += s.warp_val[0][w];
     at += in - mine;
     if (goal >= at && goal < at + mine) {
-        for (int i = i0; i < i1; ++i) {
-            const u64 w = kept(i);
+        for (int i = tid * each * 4 - pad; i < g_end * 4 - pad; ++i) {
+            const u64 w = kept_weight(r.v[i], i);
             if (goal < at + w) {
                 p.tokens[row] = c0 + i;
                 if (p.probs) p.probs[row] = (float)((double)w / (double)total);
@@ -568,11 +599,13 @@ size_t sample_smem_bytes(int vocab, int cluster)
     return ((sizeof(Shared) + 15) & ~size_t(15)) + ((size_t)per + 16) * sizeof(float);
 }
 
-// CTAs of a row: enough that its logits fit and a CTA has some 20 K of them at most (two CTAs an SM then), one per 4 K.
-int sample_cluster(int vocab)
+// CTAs of a row: one for each 4 K of its logits, up to eight (76 KB each of a vocabulary of 152 K, two CTAs an SM).  Where the rows
+// leave most SMs without work, up to sixteen.
+int sample_cluster(int vocab, int rows, int n_sm)
 {
     int c = 1;
-    while (c < kMaxCluster && vocab > c * 4096) c *= 2;
+    while (c < 8 && vocab > c * 4096) c *= 2;
+    if (c == 8 && vocab > 65536 && rows * kMaxCluster <= n_sm) c = kMaxCluster;
     return c;
 }
 
@@ -582,6 +615,7 @@ cudaError_t launch_sample(const SampleParams &p, int rows, bool bf16, bool pdl, 
     const auto kernel = bf16 ? sample_kernel<true> : sample_kernel<false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
+    if (p.cluster > 8 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * p.cluster), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
