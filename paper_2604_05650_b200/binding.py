@@ -149,11 +149,16 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
 
 
 def _addr(x) -> Optional[int]:
-    if x is None or isinstance(x, int):
+    if x is None:
+        return x
+    f = getattr(x, "data_ptr", None)      # first: what nearly all calls pass, and some pass a dozen
+    if f is not None:
+        return f()
+    if isinstance(x, int):
         return x
     if isinstance(x, np.ndarray):
         return x.ctypes.data
-    return int(x.data_ptr())
+    return int(x.data_ptr())              # (raises: neither an address nor a tensor)
 
 
 def _i32(a: Sequence[int]) -> np.ndarray:
@@ -194,6 +199,7 @@ class Context:
         if st != OK:
             raise LvspecError(st, self._lib.lvspec_last_error(None).decode())
         self._h = h
+        self._stream = 0
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -213,7 +219,9 @@ class Context:
     def set_stream(self, stream) -> None:
         """``stream``: a raw cudaStream_t address, or an object with ``cuda_stream``."""
         s = getattr(stream, "cuda_stream", stream)
-        self._check(self._lib.lvspec_set_stream(self._h, ctypes.c_void_p(int(s) if s else 0)))
+        if s != self._stream:             # a decoding loop sets the one it has before every call
+            self._check(self._lib.lvspec_set_stream(self._h, ctypes.c_void_p(int(s) if s else 0)))
+            self._stream = s
 
     def set_gpu_shared(self, shared: bool = True) -> None:
         """Other work runs on the GPU beside this context's: see ``lvspec_set_gpu_shared``."""

@@ -11,9 +11,11 @@
 //
 // Bound by memory: 2 bytes read and 1 written per element.  The rows of a block sit next to each
 // other in the slot map, so the map itself says where blocks begin: a CTA takes a window of 64 tokens of
-// one head of K or V and works through the blocks that begin in it, 16 rows (32 at head_dim 64) a step with
-// 16-byte loads; up to 128 rows, the longest block, stay in registers between the maximum and
-// the codes, so every element is read once.
+// one head of K or V and the blocks that begin in it.  A prompt's window has one or two, a decoding step's eight (the draft
+// tokens of as many requests): the CTA's eight warps form that many teams, which work side by side (one after the other, a
+// step's blocks took 22 us instead of 6).  A thread keeps four 16-byte loads in flight, and the rows it loaded
+// stay in its registers between the maximum and the codes; rows beyond those (a block of 128 shared by few warps)
+// are read once more, from L2.
 #include <cuda_fp16.h>
 
 #include "lvspec_internal.h"
@@ -30,13 +32,17 @@ constexpr int kWindow = 64;
 // Largest finite magnitude among 8 bf16 values, as bits (they order as the values do).
 __device__ __forceinline__ uint32_t finite_max(uint4 x)
 {
-    uint32_t m = 0;
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    const uint32_t w[4] = {x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu, x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu};
+    const uint32_t two = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
+    uint32_t m = max(two & 0xFFFFu, two >> 16);
+    if (m >= 0x7F80u) {                 // an infinity or a NaN among them
+        m = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const uint32_t lo = w[k] & 0x7FFFu, hi = (w[k] >> 16) & 0x7FFFu;
-        if (lo < 0x7F80u) m = max(m, lo);
-        if (hi < 0x7F80u) m = max(m, hi);
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = w[k] & 0xFFFFu, hi = w[k] >> 16;
+            if (lo < 0x7F80u) m = max(m, lo);
+            if (hi < 0x7F80u) m = max(m, hi);
+        }
     }
     return m;
 }
@@ -55,18 +61,6 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
     return pack_e4m3x2(a, b) | (pack_e4m3x2(c, d) << 16);
 }
 
-// x / s: s is a power of two unless the caller's cache came with another scale
-struct Divide {
-    float s, inv;
-    bool exact;
-    __device__ __forceinline__ Divide(float s_) : s(s_), inv(1.0f / s_)
-    {
-        const uint32_t e = (__float_as_uint(s_) >> 23) & 0xFFu;
-        exact = (__float_as_uint(s_) & 0x7FFFFFu) == 0 && e > 0 && e < 254;
-    }
-    __device__ __forceinline__ float operator()(float x) const { return exact ? x * inv : __fdiv_rn(x, s); }
-};
-
 __device__ __forceinline__ float2 decode2(uint32_t two)
 {
     uint32_t h;
@@ -75,24 +69,23 @@ __device__ __forceinline__ float2 decode2(uint32_t two)
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) append_fp8_kernel(const AppendFp8Params p)
+__global__ void __launch_bounds__(kThreads, 4) append_fp8_kernel(const AppendFp8Params p)
 {
     constexpr int kLanes = D / 8;                   // lanes of a row: 8 channels each
-    constexpr int kRows = kThreads / kLanes;        // rows of a step
-    constexpr int kSteps = 128 / kRows;             // steps that stay in registers
-    const int tid = threadIdx.x;
-    const int head = blockIdx.y;
+    constexpr int kWarpRows = 32 / kLanes;          // rows of a warp's step
+    constexpr int kSteps = 4;                       // steps that stay in registers
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const bool is_v = blockIdx.z != 0;
-    const uint16_t *src = (is_v ? p.v : p.k) + head * D;
+    const uint16_t *all_src = is_v ? p.v : p.k;
     const long long stride = is_v ? p.v_stride : p.k_stride;
-    uint8_t *pool = (is_v ? p.v_pool : p.k_pool) + head * p.head_stride;
+    uint8_t *all_pool = is_v ? p.v_pool : p.k_pool;
     float *scales = is_v ? p.v_scale : p.k_scale;
     const long long n_slots = (long long)p.n_pages * p.page_size;
     const int w0 = blockIdx.x * kWindow;
+    const int in_block = (1 << p.block_log2) - 1;
 
-    __shared__ uint32_t s_starts[kWindow / 32];
-    __shared__ int s_end, s_begun;
-    __shared__ uint32_t s_max[kWarps];
+    __shared__ uint32_t s_starts[kWindow / 32], s_breaks[kWindow / 32];
+    __shared__ uint32_t s_max[2][kWarps];
 
     grid_launch_dependents();
     grid_dependency_wait();
@@ -104,99 +97,148 @@ __global__ void __launch_bounds__(kThreads) append_fp8_kernel(const AppendFp8Par
     };
     if (tid < kWindow) {
         const int mine = block_of(w0 + tid);
-        const uint32_t starts = __ballot_sync(0xffffffffu, mine >= 0 && mine != block_of(w0 + tid - 1));
-        if ((tid & 31) == 0) s_starts[tid >> 5] = starts;
+        const bool other = mine != block_of(w0 + tid - 1);
+        const uint32_t breaks = __ballot_sync(0xffffffffu, other), starts = __ballot_sync(0xffffffffu, other && mine >= 0);
+        if (lane == 0) {
+            s_breaks[tid >> 5] = breaks;
+            s_starts[tid >> 5] = starts;
+        }
     }
     __syncthreads();
-    const uint64_t starts = s_starts[0] | ((uint64_t)s_starts[1] << 32);
-    const int row = tid / kLanes, chunk = tid % kLanes;
+    uint64_t left = s_starts[0] | ((uint64_t)s_starts[1] << 32);
+    const uint64_t breaks = s_breaks[0] | ((uint64_t)s_breaks[1] << 32);
+    // teams of 8, 4, 2 or 1 warps; team t takes the blocks t, t + teams, ...
+    const int n_blocks = __popcll(left);
+    const int team_log2 = n_blocks <= 1 ? 3 : n_blocks <= 2 ? 2 : n_blocks <= 4 ? 1 : 0;
+    const int team = warp >> team_log2, teams = kWarps >> team_log2;
+    const int row = ((warp & ((1 << team_log2) - 1)) * 32 + lane) / kLanes, chunk = lane % kLanes;
+    const int rows_step = kWarpRows << team_log2;
 
-    for (uint64_t left = starts; left; left &= left - 1) {
-        const int first = w0 + __ffsll((long long)left) - 1;
+    int turn = 0;                                   // of the two sets of words that the teams exchange
+    for (int nth = 0; left; left &= left - 1, ++nth) {
+        if (nth % teams != team) continue;
+        const int at = __ffsll((long long)left) - 1, first = w0 + at;
         const int block = block_of(first);
-        __syncthreads();
-        if (tid == 0) {
-            s_end = 0x7fffffff;
-            s_begun = 1 << p.block_log2;
+        // the run of tokens of this block: up to the next break, which may lie behind the window
+        const uint64_t later = at < 63 ? breaks >> (at + 1) : 0;
+        int end = first + __ffsll((long long)later);
+        if (!later) {
+            uint32_t other = 0;
+            for (end = w0 + kWindow; other == 0; end += 32) other = __ballot_sync(0xffffffffu, block_of(end + lane) != block);
+            end += __ffs(other) - 33;
         }
-        __syncthreads();
-        // the run of tokens of this block, and the first of the block's positions among them
-        int end, base = first;
-        do {
-            const int i = base + tid;
-            if (block_of(i) != block) atomicMin(&s_end, i);
-            __syncthreads();
-            end = s_end;
-            if (i < end) atomicMin(&s_begun, p.slot_map[i] & ((1 << p.block_log2) - 1));
-            __syncthreads();
-            base += kThreads;
-        } while (end == 0x7fffffff);
-        const int begun = s_begun, n = end - first;
-        const int pos0 = (block << p.block_log2) % p.page_size;                   // the block's first position in its page
-        const int page = (int)(((long long)block << p.block_log2) / p.page_size);
-        float *scale = scales + ((size_t)page * p.n_heads + head) * (p.page_size >> p.block_log2) + (pos0 >> p.block_log2);
-        const float had = begun > 0 ? *scale : 0.f;
-
-        uint4 x[kSteps];
-        uint32_t most = 0;
+        const int n = end - first;
+        const int slot0 = block << p.block_log2;
+        const int page = slot0 / p.page_size, pos0 = slot0 - page * p.page_size;          // the block's page, and first position in it
+        // where this thread's rows go, and the first of the block's positions among all
+        auto offset = [&](int i) { return p.slot_map[first + i] & in_block; };
+        long long to[kSteps];
+        int begun = in_block + 1;
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            const int i = u * kRows + row;
-            x[u] = make_uint4(0, 0, 0, 0);
-            if (i < n) x[u] = *reinterpret_cast<const uint4 *>(src + (first + i) * stride + chunk * 8);
+            const int i = u * rows_step + row;
+            to[u] = 0;
+            if (i < n) {
+                const int o = offset(i);
+                begun = min(begun, o);
+                to[u] = (pos0 + o) * p.position_stride;
+            }
         }
-#pragma unroll
-        for (int u = 0; u < kSteps; ++u) most = max(most, finite_max(x[u]));
-        // (more rows than a block has positions: some slot is given twice)
-        for (int i = kSteps * kRows + row; i < n; i += kRows)
-            most = max(most, finite_max(*reinterpret_cast<const uint4 *>(src + (first + i) * stride + chunk * 8)));
-        most = __reduce_max_sync(0xffffffffu, most);
-        if ((tid & 31) == 0) s_max[tid >> 5] = most;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) most = max(most, s_max[w]);
-        float now = scale_of(most);
-        if (begun > 0) now = fmaxf(now, had);
-        const Divide by(now);
+        for (int i = kSteps * rows_step + row; i < n; i += rows_step) begun = min(begun, offset(i));
+        begun = __reduce_min_sync(0xffffffffu, (uint32_t)begun);
+        const uint16_t *src0 = all_src + (first + row) * stride + chunk * 8;
+        const long long step = rows_step * stride;
+        uint8_t *dst0 = all_pool + page * p.page_stride + chunk * 8;
+        float *scale0 = scales + (size_t)page * p.n_heads * (p.page_size >> p.block_log2) + (pos0 >> p.block_log2);
 
-        uint8_t *rows = pool + page * p.page_stride;
-        auto put = [&](int i, uint4 v) {
-            const int pos = pos0 + (p.slot_map[first + i] & ((1 << p.block_log2) - 1));
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            float f[8];
+        for (int head = blockIdx.y; head < p.n_heads; head += gridDim.y, turn ^= 1) {
+            const uint16_t *src = src0 + head * D;
+            uint8_t *dst = dst0 + head * p.head_stride;
+            float *scale = scale0 + head * (p.page_size >> p.block_log2);
+            const float old = *scale;
+            uint4 x[kSteps];
+            uint32_t most = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                f[2 * k] = by(__uint_as_float(w[k] << 16));
-                f[2 * k + 1] = by(__uint_as_float(w[k] & 0xFFFF0000u));
+            for (int u = 0; u < kSteps; ++u) {
+                x[u] = make_uint4(0, 0, 0, 0);
+                if (u * rows_step + row < n) x[u] = *reinterpret_cast<const uint4 *>(src + u * step);
             }
-            *reinterpret_cast<uint2 *>(rows + pos * p.position_stride + chunk * 8) =
-                make_uint2(codes4(f[0], f[1], f[2], f[3]), codes4(f[4], f[5], f[6], f[7]));
-        };
 #pragma unroll
-        for (int u = 0; u < kSteps; ++u)
-            if (u * kRows + row < n) put(u * kRows + row, x[u]);
-        for (int i = kSteps * kRows + row; i < n; i += kRows)
-            put(i, *reinterpret_cast<const uint4 *>(src + (first + i) * stride + chunk * 8));
-        // older rows of a block whose scale grows
-        if (begun > 0 && had != now) {
-            const float ratio = __fdiv_rn(had, now);
-            for (int i = row; i < begun; i += kRows) {
-                uint2 *at = reinterpret_cast<uint2 *>(rows + (pos0 + i) * p.position_stride + chunk * 8);
-                const uint2 c = *at;
-                const float2 a = decode2(c.x), b = decode2(c.x >> 16), d = decode2(c.y), e = decode2(c.y >> 16);
-                *at = make_uint2(codes4(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio),
-                                 codes4(d.x * ratio, d.y * ratio, e.x * ratio, e.y * ratio));
+            for (int u = 0; u < kSteps; ++u) most = max(most, finite_max(x[u]));
+            for (int i = kSteps * rows_step + row; i < n; i += rows_step)
+                most = max(most, finite_max(*reinterpret_cast<const uint4 *>(src + (i - row) * stride)));
+            most = __reduce_max_sync(0xffffffffu, most);
+            if (team_log2 > 0) {
+                // maximum and first position in one word: neither takes more than 16 bits
+                uint32_t *words = s_max[turn] + (team << team_log2);
+                if (lane == 0) words[warp & ((1 << team_log2) - 1)] = (most << 16) | (uint32_t)(in_block + 1 - begun);
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 << team_log2) : "memory");
+                const uint32_t m = words[lane & ((1 << team_log2) - 1)];
+                most = __reduce_max_sync(0xffffffffu, m >> 16);
+                begun = in_block + 1 - (int)__reduce_max_sync(0xffffffffu, m & 0xFFFFu);
             }
+            float now = scale_of(most);
+            const float had = begun > 0 ? old : 0.f;
+            if (begun > 0) now = fmaxf(now, had);
+            // x / scale is x times a power of two, unless the caller's cache came with another scale
+            const uint32_t e = (__float_as_uint(now) >> 23) & 0xFFu;
+            const bool exact = (__float_as_uint(now) & 0x7FFFFFu) == 0 && e > 0 && e < 254;
+            const float inv = __uint_as_float((254u - e) << 23);
+            auto put = [&](long long to, uint4 v) {
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                float f[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    f[2 * k] = __uint_as_float(w[k] << 16);
+                    f[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+                }
+                if (exact) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) f[k] *= inv;
+                } else {
+#pragma unroll 1
+                    for (int k = 0; k < 4; ++k) {
+                        const float a = __fdiv_rn(f[0], now), b = __fdiv_rn(f[1], now);
+#pragma unroll
+                        for (int t = 0; t < 6; ++t) f[t] = f[t + 2];
+                        f[6] = a;
+                        f[7] = b;
+                    }
+                }
+                *reinterpret_cast<uint2 *>(dst + to) =
+                    make_uint2(codes4(f[0], f[1], f[2], f[3]), codes4(f[4], f[5], f[6], f[7]));
+            };
+#pragma unroll
+            for (int u = 0; u < kSteps; ++u)
+                if (u * rows_step + row < n) put(to[u], x[u]);
+            for (int i = kSteps * rows_step + row; i < n; i += rows_step)
+                put((pos0 + offset(i)) * p.position_stride, *reinterpret_cast<const uint4 *>(src + (i - row) * stride));
+            // older rows of a block whose scale grows
+            if (begun > 0 && had != now) {
+                const float ratio = __fdiv_rn(had, now);
+                for (int i = row; i < begun; i += rows_step) {
+                    uint2 *to = reinterpret_cast<uint2 *>(dst + (pos0 + i) * p.position_stride);
+                    const uint2 c = *to;
+                    const float2 a = decode2(c.x), b = decode2(c.x >> 16), d = decode2(c.y), e = decode2(c.y >> 16);
+                    *to = make_uint2(codes4(a.x * ratio, a.y * ratio, b.x * ratio, b.y * ratio),
+                                     codes4(d.x * ratio, d.y * ratio, e.x * ratio, e.y * ratio));
+                }
+            }
+            if (row == 0 && chunk == 0) *scale = now;
         }
-        if (tid == 0) *scale = now;
     }
 }
 
 }  // namespace
 
-cudaError_t launch_append_fp8(const AppendFp8Params &p, int head_dim, bool pdl, cudaStream_t stream, int *launches)
+cudaError_t launch_append_fp8(const AppendFp8Params &p, int head_dim, int n_sm, bool pdl, cudaStream_t stream, int *launches)
 {
-    const dim3 grid((unsigned)((p.n_tokens + kWindow - 1) / kWindow), (unsigned)p.n_heads, 2);
+    // a CTA for each head where tokens are few; a prompt's windows fill the device with CTAs that go through several heads (what
+    // they find out about the slots then counts for all)
+    const int windows = (p.n_tokens + kWindow - 1) / kWindow;
+    int heads = (10 * n_sm + 2 * windows - 1) / (2 * windows);
+    if (heads > p.n_heads) heads = p.n_heads;
+    const dim3 grid((unsigned)windows, (unsigned)heads, 2);
     return head_dim == 128 ? launch_after(append_fp8_kernel<128>, grid, kThreads, 0, pdl, stream, launches, p)
                            : launch_after(append_fp8_kernel<64>, grid, kThreads, 0, pdl, stream, launches, p);
 }

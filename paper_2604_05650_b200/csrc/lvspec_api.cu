@@ -1098,7 +1098,7 @@ lvspec_status_t lvspec_append_paged_fp8(lvspec_ctx_t *ctx, int32_t n_tokens, int
     p.page_size = cache->page_size;
     p.block_log2 = lay.block_log2;
     int launches = 0;
-    e = launch_append_fp8(p, head_dim, ctx->pdl, ctx->stream, &launches);
+    e = launch_append_fp8(p, head_dim, ctx->n_sm, ctx->pdl, ctx->stream, &launches);
     ctx->launches += launches;
     if (e != cudaSuccess) return cuda_fail(ctx, "cache append kernel launch", e);
     return LVSPEC_OK;

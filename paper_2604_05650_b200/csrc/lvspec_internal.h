@@ -221,7 +221,7 @@ struct AppendFp8Params {
     long long page_stride, head_stride, position_stride;     // of the pools, in bytes
     int32_t n_tokens, n_heads, n_pages, page_size, block_log2;
 };
-cudaError_t launch_append_fp8(const AppendFp8Params &p, int head_dim, bool pdl, cudaStream_t stream, int *launches);
+cudaError_t launch_append_fp8(const AppendFp8Params &p, int head_dim, int n_sm, bool pdl, cudaStream_t stream, int *launches);
 
 // Attention on a paged E4M3 cache with a scale per block (verify_attn_paged_fp8.cu).
 struct PagedFp8Params {
