@@ -68,7 +68,7 @@ __host__ __device__ constexpr bool pool_holds(int groups)
 static_assert(pool_holds(2) && pool_holds(3) && pool_holds(4), "a share of the registers that is not there is waited for without end");
 constexpr int kMergeWarps = 8;
 constexpr int kMaxBufs = 4;                 // S^T buffers and P^T buffers, at most
-constexpr float kFirst = 3.f;               // log2 of the probability of a stream's first position
+constexpr float kFirst = 6.f;               // log2 of the largest probability of a stream's first tile
 constexpr float kGuard = 14.f;              // log2 units above the reference before it moves
 constexpr int kFlatGain = 3;                // tiles a straight cut has to save to be taken
 
@@ -422,13 +422,29 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
-// Scaled scores x of eight columns: score * ck + (minus the reference)
+// A view of the references (minus them) in shared memory that the compiler may read ahead of the stores to P^T, which it could not
+// tell apart otherwise: a warp then waits for a chunk's stores before it asks for the next one's references, 200 cycles a
+// chunk instead of the 64 that its exponentials take.  Made anew (here) whenever the references may have changed.
+struct References {
+    uint32_t at;
+    __device__ __forceinline__ explicit References(const float *nm)
+    {
+        asm volatile("mov.u32 %0, %1;" : "=r"(at) : "r"(smem_u32(nm)) : "memory");
+    }
+    __device__ __forceinline__ void get8(int first, uint64_t (&n2)[4]) const
+    {
+        asm("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(n2[0]), "=l"(n2[1]) : "r"(at + 4 * first));
+        asm("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(n2[2]), "=l"(n2[3]) : "r"(at + 4 * first + 16));
+    }
+};
+
+// Scaled scores x of eight columns, from `first` on of the group's: score * ck + (minus the reference)
 template <bool kMask>
-__device__ __forceinline__ void scores8(const uint32_t *raw, const float *nm, float ck, Seen seen, int col, float (&x)[8])
+__device__ __forceinline__ void scores8(const uint32_t *raw, References nm, int first, float ck, Seen seen, int col, float (&x)[8])
 {
     const uint64_t c2 = pair(ck, ck);
-    const ulonglong2 na = *reinterpret_cast<const ulonglong2 *>(nm), nb = *reinterpret_cast<const ulonglong2 *>(nm + 4);
-    const uint64_t n2[4] = {na.x, na.y, nb.x, nb.y};
+    uint64_t n2[4];
+    nm.get8(first, n2);
 #pragma unroll
     for (int k = 0; k < 4; ++k) unpack_f32x2(fma_f32x2(pack_f32x2(raw[2 * k], raw[2 * k + 1]), c2, n2[k]), x[2 * k], x[2 * k + 1]);
     if (kMask)
@@ -438,11 +454,11 @@ __device__ __forceinline__ void scores8(const uint32_t *raw, const float *nm, fl
 
 // Eight columns of one position: probabilities into P^T and (times sign, s2) the sums.
 template <bool kMask>
-__device__ __forceinline__ void softmax8(const uint32_t *raw, const float *nm, float ck, Seen seen, int col, uint64_t v2, uint64_t s2,
-                                         float &top, float *l, uint8_t *to)
+__device__ __forceinline__ void softmax8(const uint32_t *raw, References nm, int first, float ck, Seen seen, int col, uint64_t v2,
+                                         uint64_t s2, float &top, float *l, uint8_t *to)
 {
     float x[8];
-    scores8<kMask>(raw, nm, ck, seen, col, x);
+    scores8<kMask>(raw, nm, first, ck, seen, col, x);
     top = max3(max3(top, x[0], x[1]), max3(x[2], x[3], x[4]), max3(x[5], x[6], x[7]));
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = ex2(x[k]);
@@ -477,10 +493,11 @@ __device__ __forceinline__ void tmem_ld_chunks(uint32_t taddr, uint32_t *r)
 // 170 cycles, whatever the number of columns; 16 columns' work takes 330): probabilities into P^T and (times sign) the sums;
 // returns the largest scaled score.
 template <int kC, int kBlock, bool kMask>
-__device__ __forceinline__ float softmax_pass(uint32_t s_addr, const float *nm, float ck, float vsr, Seen seen, int col0,
+__device__ __forceinline__ float softmax_pass(uint32_t s_addr, const float *nm_s, float ck, float vsr, Seen seen, int col0,
                                               uint8_t *prow, float sign, float (&l)[kC * 8])
 {
     float top = -INFINITY;
+    const References nm(nm_s);
     const uint64_t v2 = pair(vsr, vsr), s2 = pair(sign, sign);
 #pragma unroll
     for (int b = 0; b < kC; b += kBlock) {
@@ -491,7 +508,7 @@ __device__ __forceinline__ float softmax_pass(uint32_t s_addr, const float *nm, 
 #pragma unroll
         for (int u = 0; u < kBlock; ++u)
             if (b + u < kC)
-                softmax8<kMask>(raw + u * 8, nm + (b + u) * 8, ck, seen, col0 + (b + u) * 8, v2, s2, top, l + (b + u) * 8,
+                softmax8<kMask>(raw + u * 8, nm, (b + u) * 8, ck, seen, col0 + (b + u) * 8, v2, s2, top, l + (b + u) * 8,
                                 prow + (b + u) * 2048);
     }
     return top;
@@ -954,72 +971,53 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 const float ck = scale * sc[0], vs = sc[8];
                 const int ve = (int)((__float_as_uint(vs) >> 23) & 0xFFu) - 127;
                 if (__builtin_expect(begins, 0)) {
-                    // the first position's scores set the references, its block's V scale the scales'
-                    if (wq == 0) {
-#pragma unroll 1
-                        for (int c = 0; c < kC; ++c) {
-                            uint32_t r[8];
-                            tmem_ld_x8(s_addr + c * 8, r);
-                            tmem_wait_ld();
-                            if (lane == 0)
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) {
-                                    const float y = __uint_as_float(r[k]) * ck;
-                                    nm[c * 8 + k] = fabsf(y) < INFINITY ? kFirst - y : 0.f;
-                                }
-                        }
-                        if (lane == 0) wmax_s[4 * kGroups + grp] = (uint32_t)(ve > -127 && ve < 128 ? max(-100, min(100, ve)) + 127 : 127);
-                    }
+                    // the first tile's maxima set the references (below)
+                    if (gtid < kC * 8) nm[gtid] = 0.f;
                     named_sync(bar_id, 128);
-                    k0 = (int)wmax_s[4 * kGroups + grp] - 127 + 2;
-                    inv_k0 = pow2(-k0);
                 }
                 uint8_t *prow = gbase + sm.p + place(n, sm.p_log2) * (NP * 256) + c_lo * 2048 + row * 16;
-                // A pass is taken back and made again when a score passes the guard, a V scale is large against 2^k0, or the
-                // stream begins in the draft slots, where its first position need not be one that every query sees.
+                const Seen seen = tail ? seen_by(pos - (L - gamma), G, gamma, p.branch_len) : Seen{0, 0xFFFFFFFFu};
+                // A stream's first tile sets its references: to the tile's maxima, 2^kFirst below the largest probability.  They move when
+                // a score of a later tile passes the guard or a V scale is large against 2^k0: the tile's pass is taken back and made
+                // again.
+                bool move = begins, back = false;
 #pragma unroll 1
-                for (int turn = 0, back = 0;;) {
-                    float top;
-                    const float vsr = vs * inv_k0, sign = back ? -1.f : 1.f;
-                    if (__builtin_expect(!tail, 1)) {
-                        const Seen all = {0, 0xFFFFFFFFu};
-                        top = softmax_pass<kC, kBlock, false>(s_addr, nm, ck, vsr, all, col0, prow, sign, l);
-                    } else {
-                        const Seen seen = seen_by(pos - (L - gamma), G, gamma, p.branch_len);
-                        top = softmax_pass<kC, kBlock, true>(s_addr, nm, ck, vsr, seen, col0, prow, sign, l);
-                    }
-                    if (!back) {
-                        // (all of the group's P^T is on its way to the tensor core when the vote is over)
-                        tc_fence_before();
-                        fence_proxy_async_smem();
-                        const bool beyond = top > kGuard || (ve > k0 && ve < 100) || (begins && tail && turn == 0);
-                        if (__builtin_expect(!group_any(bar_id, beyond) || turn == 3, 1)) break;
-                        // this tile's maxima over the lanes
-                        const Seen seen = seen_by(pos - (L - gamma), G, gamma, p.branch_len);
-                        const int e = __reduce_max_sync(0xffffffffu, ve < 128 ? min(ve, 100) : -127);
-#pragma unroll 1
-                        for (int c = 0; c < kC; ++c) {
-                            uint32_t r[8];
-                            tmem_ld_x8(s_addr + c * 8, r);
-                            tmem_wait_ld();
-                            float x[8];
-                            scores8<true>(r, nm + c * 8, ck, seen, col0 + c * 8, x);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const float y = warp_max_f32(x[k]);
-                                if (lane == 0) tmx[wq * NP + c * 8 + k] = y;
-                            }
+                for (int turn = 0;;) {
+                    if (!move) {
+                        const float vsr = vs * inv_k0, sign = back ? -1.f : 1.f;
+                        const float top = __builtin_expect(!tail, 1)
+                                              ? softmax_pass<kC, kBlock, false>(s_addr, nm, ck, vsr, seen, col0, prow, sign, l)
+                                              : softmax_pass<kC, kBlock, true>(s_addr, nm, ck, vsr, seen, col0, prow, sign, l);
+                        if (!back) {
+                            // (all of the group's P^T is on its way to the tensor core when the vote is over)
+                            tc_fence_before();
+                            fence_proxy_async_smem();
+                            if (__builtin_expect(!group_any(bar_id, top > kGuard || (ve > k0 && ve < 100)) || turn == 3, 1)) break;
+                            back = true;
+                            ++turn;
+                            continue;
                         }
-                        if (lane == 0) wmax_s[warp - kSoftmaxWarp0] = (uint32_t)(e + 127);
-                        back = 1;
-                        ++turn;
-                        continue;
                     }
-                    // ---- the sums are without this tile again: references up to its maxima
+                    // ---- references up to this tile's maxima over the lanes (the sums are without this tile)
+                    int e = __reduce_max_sync(0xffffffffu, ve < 128 ? min(ve, 100) : -127);
+                    const References refs(nm);
+#pragma unroll 1
+                    for (int c = 0; c < kC; ++c) {
+                        uint32_t r[8];
+                        tmem_ld_x8(s_addr + c * 8, r);
+                        tmem_wait_ld();
+                        float x[8];
+                        scores8<true>(r, refs, c * 8, ck, seen, col0 + c * 8, x);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float y = warp_max_f32(x[k]);
+                            if (lane == 0) tmx[wq * NP + c * 8 + k] = y;
+                        }
+                    }
+                    if (lane == 0) wmax_s[warp - kSoftmaxWarp0] = (uint32_t)(e + 127);
                     named_sync(bar_id, 128);
-                    const int e = (int)__reduce_max_sync(0xffffffffu, wmax_s[grp * 4 + (lane & 3)]) - 127;
-                    const int k_new = e > k0 ? e + 2 : k0;
-                    const float fk = pow2(max(k0 - k_new, -126));
+                    e = max(-100, (int)__reduce_max_sync(0xffffffffu, wmax_s[grp * 4 + (lane & 3)]) - 127);
+                    const int k_new = begins && turn == 0 ? e + 2 : e > k0 ? e + 2 : k0;
                     if (gtid < kC * 8) {
                         const float t = fmaxf(fmaxf(tmx[gtid], tmx[NP + gtid]), fmaxf(tmx[2 * NP + gtid], tmx[3 * NP + gtid]));
                         const float up = (begins ? t > -INFINITY : t > kGuard) ? t - kFirst : 0.f;
@@ -1027,15 +1025,13 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                         fac[gtid] = ex2(-up);
                     }
                     named_sync(bar_id, 128);
-#pragma unroll
-                    for (int c = 0; c < kC; ++c)
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                // (NaN: the tile had brought an infinity, against which what was there before does not count)
-                                const float y = l[c * 8 + k];
-                                l[c * 8 + k] = y == y ? y * fac[c * 8 + k] : 0.f;
-                            }
                     if (!begins) {
+                        const float fk = pow2(max(k0 - k_new, -126));
+#pragma unroll
+                        for (int k = 0; k < kC * 8; ++k) {
+                            // (NaN: the tile had brought an infinity, against which what was there before does not count)
+                            l[k] = l[k] == l[k] ? l[k] * fac[k] : 0.f;
+                        }
                         // (the products of the stream's last tile have ended; the next are those of this one)
                         wait(pv_done(last), round_of(last, sm.p_log2), abort_flag);
                         __syncwarp();
@@ -1051,18 +1047,20 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                             tmem_st_x8(o_addr, o);
                         }
                         tmem_wait_st();
+                        for (int c = lane; c < kC * 8; c += 32) {
+                            my_sums[c] *= fac[c];
+                            my_sums[4 * NP + c] *= fac[c];
+                        }
+                        __syncwarp();
+                    } else if (turn > 0) {
+#pragma unroll
+                        for (int k = 0; k < kC * 8; ++k) l[k] = 0.f;
                     }
-                    for (int c = lane; c < kC * 8; c += 32) {
-                        my_sums[c] *= fac[c];
-                        my_sums[4 * NP + c] *= fac[c];
-                    }
-                    __syncwarp();
                     k0 = k_new;
                     inv_k0 = pow2(-k0);
-                    back = 0;
+                    move = back = false;
                 }
                 if (__builtin_expect(!inside && pos0 + kTilePos > vis0 && pos0 < vis1, 0)) {
-                    const Seen seen = seen_by(pos - (L - gamma), G, gamma, p.branch_len);
                     const bool in = pos >= vis0 && pos < vis1;
 #pragma unroll 1
                     for (int c = 0; c < kC; ++c) {
@@ -1070,7 +1068,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                         tmem_ld_x8(s_addr + c * 8, r);
                         tmem_wait_ld();
                         float x[8];
-                        scores8<true>(r, nm + c * 8, ck, seen, col0 + c * 8, x);
+                        scores8<true>(r, References(nm), c * 8, ck, seen, col0 + c * 8, x);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) x[k] = in ? ex2(x[k]) : 0.f;
                         add_to_sums(c, warp_sums(x, lane), false, true);
