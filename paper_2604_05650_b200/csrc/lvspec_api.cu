@@ -1217,6 +1217,7 @@ lvspec_status_t lvspec_verify_attention_paged_fp8(lvspec_ctx_t *ctx, const lvspe
     if (st != LVSPEC_OK) return st;
     p.part_o = static_cast<float *>(ctx->scratch);
     p.part_stat = p.part_o + (size_t)2 * p.n_cta * p.M * p.D;
+    p.line = reinterpret_cast<int32_t *>(p.part_stat + (size_t)2 * p.n_cta * p.M * 4);
     int launches = 0;
     e = launch_attn_paged_fp8(p, static_cast<const uint8_t *>(k_pool), static_cast<const uint8_t *>(v_pool), ctx->stream, &launches);
     ctx->launches += launches;

@@ -229,6 +229,7 @@ struct PagedFp8Params {
     uint16_t *out;                      // the same
     float *mass;                        // [B, gamma, Hq]
     float *part_o, *part_stat;          // [2 n_cta, M, D] and [2 n_cta, M, 4]: m (log2 units), l, l_vis, unused
+    int32_t *line;                      // how the tiles were shared out, for the merge: share, aligned, then {start, length} by sequence
     uint32_t *status;
     const int32_t *block_table, *kv_len, *span;
     const float *k_scale, *v_scale;     // [n_pages, Hkv, blocks_per_page]

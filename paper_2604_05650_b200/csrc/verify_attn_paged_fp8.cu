@@ -580,7 +580,13 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         grid_dependency_wait();
         grid_launch_dependents();
         const bool bad = make_line(line, p.kv_len, p.B, p.Hkv, p.max_len, p.n_cta);
-        if (bad && blockIdx.x == 0 && lane == 0) atomicOr(p.status, LVSPEC_DEV_BAD_LENGTH);
+        if (blockIdx.x == 0) {
+            if (bad && lane == 0) atomicOr(p.status, LVSPEC_DEV_BAD_LENGTH);
+            // (the merge looks it up instead of working it out again)
+            __syncwarp();
+            if (lane < 2) p.line[lane] = lane ? line.aligned : line.share;
+            for (int b = lane; b < p.B; b += 32) *reinterpret_cast<int2 *>(p.line + 2 + 2 * b) = make_int2(line.start[b], line.len[b]);
+        }
     } else {
         if (warp == 1) {
             tmem_alloc(base + sm.misc, (uint32_t)P.tmem_cols);
@@ -1172,71 +1178,77 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
 
 // Merges the parts of pairs that several CTAs share: one warp per query row.  With m, l and the unnormalised O of
 // each part, w = 2^(m - max m): out = sum w O / sum w l, mass = sum w l_vis / sum w l, summed in the CTAs' order.
-// Rows of empty sequences are written as zeros here.
+// Rows of empty sequences are written as zeros here.  All latency (40 rows of 8 heads, 19 parts each: 3.1 MB from L2): the first
+// sixteen parts are asked for together with the statistics that say what they weigh.
 template <int D>
 __global__ void __launch_bounds__(32 * kMergeWarps) merge_paged_fp8_kernel(const PagedFp8Params p, const uint32_t group_magic)
 {
-    __shared__ Line line;
-    constexpr int kEach = D / 32;
+    constexpr int kEach = D / 32, kAhead = 16;
     using Vec = typename std::conditional<D == 128, float4, float2>::type;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    grid_launch_dependents();
-    grid_dependency_wait();
-    if (warp == 0) make_line(line, p.kv_len, p.B, p.Hkv, p.max_len, p.n_cta);
-    __syncthreads();
     const int row = blockIdx.x * kMergeWarps + warp;
-    if (row >= p.B * p.gamma * p.Hq) return;
     const int b = row / (p.gamma * p.Hq), r = row - b * p.gamma * p.Hq, g = r / p.Hq, h = r - g * p.Hq;
     const int head = div_by(h, p.G, group_magic), col = g * p.G + h - head * p.G;
-    uint16_t *out = p.out + (size_t)row * D + lane * kEach;
-    const int tiles = tiles_of(line.len[b]);
+    grid_launch_dependents();
+    grid_dependency_wait();
+    if (b >= p.B) return;
+    const int2 cut = *reinterpret_cast<const int2 *>(p.line), seq = *reinterpret_cast<const int2 *>(p.line + 2 + 2 * b);
+    const int share = cut.x, tiles = tiles_of(seq.y);
     float acc[kEach] = {};
-    float inv = 0.f, mass = 0.f;
+    float total = 0.f, vis = 0.f;
     if (tiles > 0) {
-        const int first = line.start[b] + head * padded(line, tiles);
-        const int c0 = first / line.share, c1 = (first + tiles - 1) / line.share;
-        if (c0 == c1) return;                           // that CTA has finished the pair itself
-        auto stat = [&](int c) { return *reinterpret_cast<const float4 *>(p.part_stat + ((size_t)part_slot(c, c == c0) * p.M + col) * 4); };
-        float top = -INFINITY;
-        for (int c = c0 + lane; c <= c1; c += 32) {
-            const float4 s = stat(c);
+        const int first = seq.x + head * (cut.y ? (tiles + share - 1) / share * share : tiles);
+        const int c0 = first / share, n = (first + tiles - 1) / share - c0 + 1;
+        if (n == 1) return;                             // that CTA has finished the pair itself
+        auto at = [&](int u) { return (size_t)part_slot(c0 + u, u == 0) * p.M + col; };
+        auto values = [&](int u) { return *reinterpret_cast<const Vec *>(p.part_o + at(u) * D + lane * kEach); };
+        auto stat = [&](int u) { return u < n ? *reinterpret_cast<const float4 *>(p.part_stat + at(u) * 4) : make_float4(0.f, 0.f, 0.f, 0.f); };
+        const float4 mine = stat(lane);
+        Vec v[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (u < n) v[u] = values(u);
+        float top = mine.y != 0.f ? mine.x : -INFINITY;
+        for (int u = 32 + lane; u < n; u += 32) {
+            const float4 s = stat(u);
             if (s.y != 0.f) top = fmaxf(top, s.x);
         }
         top = warp_max_f32(top);
-        float total = 0.f, vis = 0.f;
-        for (int cb = c0; cb <= c1; cb += 32) {
-            float w = 0.f, wl = 0.f, wv = 0.f;
-            if (cb + lane <= c1) {
-                const float4 s = stat(cb + lane);
-                if (s.y != 0.f) w = ex2(s.x - top);     // (a part that the row sees nothing of counts for nothing)
-                wl = w * s.y;
-                wv = w * s.z;
-            }
+        float wl = 0.f, wv = 0.f;
+        for (int u0 = 0; u0 < n; u0 += 32) {
+            const float4 s = u0 == 0 ? mine : stat(u0 + lane);
+            const float w = s.y != 0.f ? ex2(s.x - top) : 0.f;      // (a part that the row sees nothing of counts for nothing)
+            wl = fmaf(w, s.y, wl);
+            wv = fmaf(w, s.z, wv);
+            for (int u1 = 0; u1 < 32 && u0 + u1 < n; u1 += kAhead) {
+                if (u0 + u1 > 0)
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                wl += __shfl_xor_sync(0xffffffffu, wl, o);
-                wv += __shfl_xor_sync(0xffffffffu, wv, o);
-            }
-            total += wl;
-            vis += wv;
-            const int n = min(32, c1 - cb + 1);
-#pragma unroll 4
-            for (int u = 0; u < n; ++u) {
-                const float wu = __shfl_sync(0xffffffffu, w, u);
-                if (wu == 0.f) continue;
-                const Vec v = *reinterpret_cast<const Vec *>(p.part_o + ((size_t)part_slot(cb + u, cb + u == c0) * p.M + col) * D + lane * kEach);
-                const float *f = reinterpret_cast<const float *>(&v);
+                    for (int u = 0; u < kAhead; ++u)
+                        if (u0 + u1 + u < n) v[u] = values(u0 + u1 + u);
 #pragma unroll
-                for (int k = 0; k < kEach; ++k) acc[k] = fmaf(wu, f[k], acc[k]);
+                for (int u = 0; u < kAhead; ++u) {
+                    const float wu = __shfl_sync(0xffffffffu, w, u1 + u);
+                    if (wu == 0.f) continue;            // (beyond the last part too)
+                    const float *f = reinterpret_cast<const float *>(&v[u]);
+#pragma unroll
+                    for (int k = 0; k < kEach; ++k) acc[k] = fmaf(wu, f[k], acc[k]);
+                }
             }
         }
-        inv = total == 0.f ? 0.f : 1.f / total;
-        mass = vis * inv;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            wl += __shfl_xor_sync(0xffffffffu, wl, o);
+            wv += __shfl_xor_sync(0xffffffffu, wv, o);
+        }
+        total = wl;
+        vis = wv;
     }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    uint16_t *out = p.out + (size_t)row * D + lane * kEach;
 #pragma unroll
     for (int k = 0; k < kEach; k += 2)
         *reinterpret_cast<uint32_t *>(out + k) = pack_bf16x2(acc[k] * inv, acc[k + 1] * inv);
-    if (lane == 0) p.mass[row] = mass;
+    if (lane == 0) p.mass[row] = vis * inv;
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -1276,7 +1288,10 @@ cudaError_t launch_attention(const KernelParams &P, const CUtensorMap &tk, const
 
 }  // namespace
 
-size_t paged_fp8_scratch_bytes(int n_cta, int M, int D) { return (size_t)2 * n_cta * M * (D + 4) * sizeof(float); }
+size_t paged_fp8_scratch_bytes(int n_cta, int M, int D)
+{
+    return (size_t)2 * n_cta * M * (D + 4) * sizeof(float) + (2 + 2 * LVSPEC_MAX_BATCH) * sizeof(int32_t);
+}
 
 cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool, const uint8_t *v_pool, cudaStream_t stream,
                                   int *launches)
