@@ -86,9 +86,6 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const PagePlanParam
         s_refused = 0;
     }
     __syncthreads();
-    // all inputs of this CTA have been read: the last CTA to say so may overwrite them
-    if (tid == 0) s_last = gridDim.x == 1 || atomicAdd(p.ticket, 1u) == gridDim.x - 1;
-
     // sums in 64 bits: a request may ask for anything
     long long mine = 0, first, total;
 #pragma unroll
@@ -113,6 +110,15 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const PagePlanParam
     if (tid == 0) start_s[p.batch] = (int32_t)min(total, 0x7fffffffll);
     const long long n_tokens = total;
     long long upto = block_exclusive(mine, warp_sums, total);
+    // all inputs of this CTA have been read (the sums are made of them): the last CTA to say so may overwrite them
+    if (tid == 0) {
+        s_last = 1;
+        if (gridDim.x > 1) {
+            __threadfence();
+            s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+            __threadfence();
+        }
+    }
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
         const int b = tid * kPer + u;
