@@ -1175,6 +1175,7 @@ lvspec_status_t lvspec_verify_attention_paged_fp8(lvspec_ctx_t *ctx, const lvspe
         return fail(ctx, LVSPEC_ERR_INVALID_ARG, "kv_capacity must be a whole number of pages");
     if (max_kv_len < 1 || max_kv_len > shape->kv_capacity)
         return fail(ctx, LVSPEC_ERR_INVALID_ARG, "max_kv_len outside 1..kv_capacity");
+    if (max_kv_len > (1 << 30)) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "max_kv_len beyond 2^30");
     const int64_t tiles = (int64_t)shape->batch * shape->n_kv_heads * (((int64_t)max_kv_len + 127) / 128);
     if (tiles > (int64_t(1) << 30)) return fail(ctx, LVSPEC_ERR_INVALID_ARG, "batch * n_kv_heads * max_kv_len out of range");
     if (!aligned4(k_scale) || !aligned4(v_scale) || !aligned4(block_table) || !aligned4(kv_len) || !aligned4(visual_span))

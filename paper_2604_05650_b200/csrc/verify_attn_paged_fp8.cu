@@ -904,9 +904,28 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 if (lane == 0) wmax_s[warp - kSoftmaxWarp0] = amax;
                 named_sync(kAll, kSoftmaxThreads);
                 amax = __reduce_max_sync(0xffffffffu, lane < 4 * kGroups ? wmax_s[lane] : 0u);
-                // the power of two that brings the largest magnitude into [128, 256); NaN or Inf in q: none, the result is NaN
+                if (__builtin_expect(amax >= 0x7F80u, 0)) {
+                    // NaN or Inf: its row's results are NaN, and the others are scaled by what is finite
+                    amax = 0;
+#pragma unroll 1
+                    for (int ch = stid; ch < n_chunks; ch += kSoftmaxThreads) {
+                        const uint4 x = load(ch);
+                        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const uint32_t a = (w[k >> 1] >> (16 * (k & 1))) & 0x7FFFu;
+                            if (a < 0x7F80u) amax = max(amax, a);
+                        }
+                    }
+                    amax = __reduce_max_sync(0xffffffffu, amax);
+                    named_sync(kAll, kSoftmaxThreads);
+                    if (lane == 0) wmax_s[warp - kSoftmaxWarp0] = amax;
+                    named_sync(kAll, kSoftmaxThreads);
+                    amax = __reduce_max_sync(0xffffffffu, lane < 4 * kGroups ? wmax_s[lane] : 0u);
+                }
+                // the power of two that brings the largest magnitude into [128, 256)
                 int shift = 0;
-                if (amax > 0 && amax < 0x7F80u) shift = 7 - ((int)(amax >> 7) - 127);
+                if (amax > 0) shift = 7 - ((int)(amax >> 7) - 127);
                 shift = max(-100, min(100, shift));
                 const float up = pow2(shift);
                 scale = p.scale_log2 * pow2(-shift);
