@@ -26,7 +26,9 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;
-constexpr int kCandidates = 1024;       // tokens of a bin that are ranked directly
+constexpr int kCandidates = 1024;       // tokens that are ranked directly
+constexpr int kRankAlone = 160;         // up to so many each CTA ranks all, beyond they share the work
+constexpr int kListed = 2 * kBins / kWarps;         // tokens in a warp's list
 constexpr int kMaxCluster = 16;
 typedef unsigned long long u64;
 
@@ -106,29 +108,46 @@ struct Place {
 struct Shared {
     u64 box[2][kMaxCluster][4];         // what the CTAs tell one another, two rounds by turns
     u64 warp_val[3][kWarps];
-    uint32_t bins[kBins], all_bins[kBins];      // a histogram of this CTA's tokens, of the whole row's
+    union {
+        uint32_t bins[kBins];           // a histogram of this CTA's tokens
+        uint16_t list[kWarps][kListed]; // later the places of those that may be kept, each warp's in its order
+    };
+    uint32_t all_bins[kBins];           // the histogram of the whole row
     u64 cand[kCandidates], cand_weight[kCandidates];    // key and index of a bin's tokens; their weights
     u64 cum;
     int bin, n_cand, answer;
-    Place place;
+    u64 place, found;                   // a place as one word (key above, index below); is there one
 };
 
 struct Row {
     Shared &s;
     const float *v;                     // this CTA's logits, v[0 .. n); before and behind them, to 16-byte borders, -inf
     int n, first, pad;                  // first: the index of v[0]; pad: logits from the first border to v[0]
+    int g0, g1;                         // the warp's share of them: groups of four from the first border
+    int listed;                         // tokens in the warp's list; -1: it has none, passes go over its share
     int n_cta, rank, turn;
     Weight weight;
-    float bins_per;                     // 32 / T
+    float bins_per, bin_step;           // 64 / T and its inverse
 
-    __device__ __forceinline__ Row(Shared &s_) : s(s_), turn(0) {}
+    __device__ __forceinline__ Row(Shared &s_) : s(s_), listed(-1), turn(0) {}
 
-    // f(logit, its place in v) for this CTA's logits above -inf, four side by side
+    // f(logit, its place in v) for the warp's logits above -inf, or those of its list
     template <typename F>
     __device__ __forceinline__ void for_each(F f) const
     {
+        const int lane = threadIdx.x & 31;
+        if (listed >= 0) {
+            const uint16_t *list = s.list[threadIdx.x >> 5];
+#pragma unroll 1
+            for (int e = lane; e < listed; e += 32) {
+                const int i = list[e];
+                f(v[i], i);
+            }
+            return;
+        }
         const float4 *g4 = reinterpret_cast<const float4 *>(v - pad);
-        for (int g = threadIdx.x; g * 4 < pad + n; g += kThreads) {
+#pragma unroll 1
+        for (int g = g0 + lane; g < g1; g += 32) {
             const float4 x = g4[g];
             const float l[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -136,6 +155,39 @@ struct Row {
                 if (l[k] > -INFINITY) f(l[k], g * 4 + k - pad);
         }
     }
+    // Lists the warp's logits from `least` on, in their order.  A warp with more than it has room for goes on without a list.  (The
+    // bins are the lists' memory: no CTA may need them any more.)
+    __device__ void make_list(float least)
+    {
+        if (!(least > -INFINITY)) return;
+        const int lane = threadIdx.x & 31;
+        uint16_t *list = s.list[threadIdx.x >> 5];
+        const float4 *g4 = reinterpret_cast<const float4 *>(v - pad);
+        const uint32_t below = (1u << lane) - 1u;
+        int m = 0;
+#pragma unroll 1
+        for (int g = g0; g < g1; g += 32) {
+            const float4 x = g + lane < g1 ? g4[g + lane] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            const float l[4] = {x.x, x.y, x.z, x.w};
+            if (!__any_sync(0xffffffffu, fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])) >= least)) continue;
+            int at = m, all = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t has = __ballot_sync(0xffffffffu, l[k] >= least);
+                at += __popc(has & below);
+                all += __popc(has);
+            }
+            if (m + all > kListed) return;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (l[k] >= least) list[at++] = (uint16_t)((g + lane) * 4 + k - pad);
+            m += all;
+        }
+        __syncwarp();
+        listed = m;
+    }
+    // No logit of bins 0 .. bin is below this.
+    __device__ __forceinline__ float least_of(int bin) const { return bin < kBins - 1 ? weight.top - (float)(bin + 1) * bin_step : -INFINITY; }
 
     // Sums (op 0), or largest values (op 1), of kN numbers per thread over the row; every CTA's in box[slot].
     template <int kN>
@@ -173,7 +225,15 @@ struct Row {
     __device__ u64 of_all(int slot, int k, int op)
     {
         u64 t = 0;
-        for (int r = 0; r < n_cta; ++r) {
+        int r = 0;
+        for (; r + 4 <= n_cta; r += 4) {
+            u64 y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = s.box[slot][r + j][k];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t = op ? (y[j] > t ? y[j] : t) : t + y[j];
+        }
+        for (; r < n_cta; ++r) {
             const u64 y = s.box[slot][r][k];
             t = op ? (y > t ? y : t) : t + y;
         }
@@ -186,7 +246,7 @@ struct Row {
         return (int)(__float_as_uint(t + 12582912.f) - 0x4B400000u);          // (1.5 * 2^23: the integer is in the low bits)
     }
     // Weight of a logit in the middle of a bin (none for the last, which has no end)
-    __device__ __forceinline__ u64 bin_weight(int b) const { return b < kBins - 1 ? weight(weight.top - b / bins_per) : 0; }
+    __device__ __forceinline__ u64 bin_weight(int b) const { return b < kBins - 1 ? weight(weight.top - b * bin_step) : 0; }
     // Bins of the whole row from those of the CTAs (which a cluster barrier has seen done): each CTA adds up its share and hands it
     // to all.
     __device__ void share_bins()
@@ -195,8 +255,15 @@ struct Row {
         for (int i = threadIdx.x; i < per / 2; i += kThreads) {
             const int bin = rank * per + 2 * i;
             u64 c = 0;                  // two 32-bit counters side by side: neither overflows
-            for (int r = 0; r < n_cta; ++r) c += ld_peer(peer_address(ptx::smem_u32(&s.bins[bin]), r));
-            for (int r = 0; r < n_cta; ++r) st_peer(peer_address(ptx::smem_u32(&s.all_bins[bin]), r), c);
+            int r = 0;
+            for (; r + 4 <= n_cta; r += 4) {
+                u64 y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = ld_peer(peer_address(ptx::smem_u32(&s.bins[bin]), r + j));
+                c += (y[0] + y[1]) + (y[2] + y[3]);
+            }
+            for (; r < n_cta; ++r) c += ld_peer(peer_address(ptx::smem_u32(&s.bins[bin]), r));
+            for (r = 0; r < n_cta; ++r) st_peer(peer_address(ptx::smem_u32(&s.all_bins[bin]), r), c);
         }
         cluster_sync();
     }
@@ -229,7 +296,8 @@ struct Row {
         if (tid == 0) s.bin = kBins;
         __syncthreads();
         u64 at = in - mine;
-        for (int w = 0; w < warp; ++w) at += s.warp_val[0][w];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) at += w < warp ? s.warp_val[0][w] : 0;
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
             if (at < want && at + a[k] >= want) {
@@ -246,13 +314,15 @@ struct Row {
     }
 
     // Puts a bin right by exact sums of the row's weights: the one in which the running sum over the bins reaches `need`.  `bin_at`
-    // says which bin of 0..kBins - 1 a logit is in (-1: none).  `before`: the sum of the bins before it; `count`: its tokens.
+    // says which bin of 0..kBins - 1 a logit is in (-1: none); the lists, if any, hold bins up to `b_listed`.  `before`: the sum of the
+    // bins before it; `count`: its tokens.
     template <typename BinAt>
-    __device__ int settle(int b, u64 need, u64 &before, u64 &count, BinAt bin_at)
+    __device__ int settle(int b, int b_listed, u64 need, u64 &before, u64 &count, BinAt bin_at)
     {
         if (b >= kBins) b = kBins - 1;
         int lo = 0, hi = kBins - 1;
         for (int turn_no = 0;; ++turn_no) {
+            if (b > b_listed) listed = -1;
             u64 above = 0, inside = 0, tokens = 0;
             for_each([&](float l, int) {
                 const int bb = bin_at(l);
@@ -276,6 +346,62 @@ struct Row {
         }
     }
 
+    // Gives a token of the candidates to all CTAs; places are handed out by the first.
+    __device__ __forceinline__ void put_candidate(float l, int i, u64 w)
+    {
+        const uint32_t at = add_peer(peer_address(ptx::smem_u32(&s.n_cand), 0), 1u);
+        if (at >= kCandidates) return;          // (never: they have been counted)
+        const u64 word = ((u64)key_of(l) << 32) | (0xFFFFFFFFu - (uint32_t)(first + i));
+        for (int r = 0; r < n_cta; ++r) {
+            st_peer(peer_address(ptx::smem_u32(&s.cand[at]), r), word);
+            st_peer(peer_address(ptx::smem_u32(&s.cand_weight[at]), r), w);
+        }
+    }
+    // The one of m candidates at which the running sum in their order reaches `need`; false if none does.  (A cluster barrier
+    // has seen them there.)
+    __device__ bool rank_candidates(int m, u64 need, Place &place)
+    {
+        const int tid = threadIdx.x;
+        if (tid == 0) s.n_cand = 0;
+        // larger words come first; lanes side by side share a candidate's comparisons
+        const bool shared = m > kRankAlone && n_cta > 1;
+        const int by = shared ? n_cta : 1, c_of = shared ? rank : 0, own = (m - c_of + by - 1) / by;
+        int side = 1;
+        while (side < 32 && side * 2 * own <= kThreads) side *= 2;
+        for (int c0 = 0; c0 < own; c0 += kThreads / side) {
+            const int c = (c0 + tid / side) * by + c_of;
+            const u64 mine = c < m ? s.cand[c] : 0;
+            u64 sum = 0;
+            if (c < m) {
+#pragma unroll 4
+                for (int j = tid % side; j < m; j += side)
+                    if (s.cand[j] > mine) sum += s.cand_weight[j];
+            }
+            for (int o = side / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (c < m && tid % side == 0 && sum < need && sum + s.cand_weight[c] >= need) {
+                if (!shared) {
+                    s.place = mine;
+                    s.found = 1;
+                } else {
+                    for (int r = 0; r < n_cta; ++r) {
+                        st_peer(peer_address(ptx::smem_u32(&s.place), r), mine);
+                        st_peer(peer_address(ptx::smem_u32(&s.found), r), 1);
+                    }
+                }
+            }
+        }
+        if (shared) cluster_sync();
+        else __syncthreads();
+        const bool found = s.found != 0;
+        if (found) {
+            place.key = (uint32_t)(s.place >> 32);
+            place.index = (int)(0xFFFFFFFFu - (uint32_t)s.place);
+        }
+        __syncthreads();
+        if (tid == 0) s.found = 0;              // (a cluster barrier comes before the next candidates)
+        return found;
+    }
+
     // The last token of the prefix: of the `total` tokens of bin `bin` of (M - l), the one at which the count (by_mass = false) or
     // the sum of weights reaches `need`, counted from the bin's first.
     __device__ Place resolve(int bin, bool by_mass, u64 need, u64 total)
@@ -288,40 +414,13 @@ struct Row {
         };
         for (;;) {
             if (total <= kCandidates) {
-                // ---- rank them all: places in the list are handed out by the first CTA
-                const uint32_t counter = peer_address(ptx::smem_u32(&s.n_cand), 0);
                 for_each([&](float l, int i) {
                     uint32_t k;
-                    if (!in_bin(l, k)) return;
-                    const uint32_t at = add_peer(counter, 1u);
-                    const u64 w = by_mass ? weight(l) : 1;
-                    for (int r = 0; r < n_cta; ++r) {
-                        st_peer(peer_address(ptx::smem_u32(&s.cand[at]), r), ((u64)k << 32) | (0xFFFFFFFFu - (uint32_t)(first + i)));
-                        st_peer(peer_address(ptx::smem_u32(&s.cand_weight[at]), r), w);
-                    }
+                    if (in_bin(l, k)) put_candidate(l, i, by_mass ? weight(l) : 1);
                 });
                 cluster_sync();
-                if (tid == 0) s.n_cand = 0;
-                // larger words come first; lanes side by side share a candidate's comparisons
-                const int m = (int)total;
-                int side = 1;
-                while (side < 32 && side * 2 * m <= kThreads) side *= 2;
-                for (int c0 = 0; c0 < m; c0 += kThreads / side) {
-                    const int c = c0 + tid / side;
-                    const u64 mine = c < m ? s.cand[c] : 0;
-                    u64 sum = 0;
-                    if (c < m)
-                        for (int j = tid % side; j < m; j += side)
-                            if (s.cand[j] > mine) sum += s.cand_weight[j];
-                    for (int o = side / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    if (c < m && tid % side == 0 && sum < need && sum + s.cand_weight[c] >= need) {
-                        s.place.key = (uint32_t)(mine >> 32);
-                        s.place.index = (int)(0xFFFFFFFFu - (uint32_t)mine);
-                    }
-                }
-                __syncthreads();
-                const Place p = s.place;
-                __syncthreads();
+                Place p = {0u, 0x7fffffff};
+                rank_candidates((int)total, need, p);
                 return p;
             }
             u64 most = 0, least = 0, count = 0;
@@ -367,6 +466,8 @@ struct Row {
                 return p;
             }
             // ---- bins of the keys
+            __syncthreads();
+            listed = -1;
             int shift = 0;
             while (((k_hi - k_lo) >> shift) >= (uint32_t)kBins) ++shift;
             lo = k_lo;
@@ -386,7 +487,7 @@ struct Row {
             int b;
             if (by_mass) {
                 b = bin_reaching(need, at, [&](int k) { return weight(logit_of(k_hi - ((uint32_t)k << shift))); });
-                b = settle(b, need, at, total, key_bin);
+                b = settle(b, kBins, need, at, total, key_bin);
             } else {
                 b = bin_reaching(need, at, [](int) { return 1ull; });
                 total = s.all_bins[b];
@@ -432,19 +533,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     r.first = c0;
     bool nan_seen = false;
     float best = -INFINITY;
-    int best_i = 0x7fffffff;
-    auto take = [&](float x, int i) {
+    auto take = [&](float x) {
         // NaN ranks as -inf; -0 and 0 are one value
         if (x != x) {
             nan_seen = true;
             x = -INFINITY;
         }
-        x += 0.f;
-        if (x > best || (x == best && i < best_i)) {
-            best = x;
-            best_i = i;
-        }
-        return x;
+        best = fmaxf(best, x);
+        return x + 0.f;
     };
     const int groups = (pad + r.n + kVec - 1) / kVec;
     constexpr int kAhead = 4;           // 16-byte loads of a thread in flight
@@ -470,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
                 else if (e + k >= 0 && e + k < r.n)
                     x[k] = kBf16 ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(from)[e + k] << 16)
                                  : reinterpret_cast<const float *>(from)[e + k];
-                if (whole || (e + k >= 0 && e + k < r.n)) x[k] = take(x[k], c0 + e + k);
+                if (whole || (e + k >= 0 && e + k < r.n)) x[k] = take(x[k]);
             }
 #pragma unroll
             for (int k = 0; k < kVec; k += 4)
@@ -478,17 +574,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         }
     }
     if (nan_seen) atomicOr(p.status, LVSPEC_DEV_NAN_LOGIT);
-    if (tid == 0) s.n_cand = 0;
+    if (tid == 0) s.n_cand = 0, s.found = 0;
     r.clear_bins();
-    // largest logit, at its lowest index
-    const u64 first_best = best_i == 0x7fffffff ? 0 : ((u64)key_of(best) << 32) | (0xFFFFFFFFu - (uint32_t)best_i);
-    const u64 largest = r.of_all(r.gather<1>(first_best, 0, 0, 1), 0, 1);
-    const float top = logit_of((uint32_t)(largest >> 32));
-    const int top_i = (int)(0xFFFFFFFFu - (uint32_t)largest);
+    const int n4 = (pad + r.n + 3) / 4, share = (n4 + kWarps - 1) / kWarps;
+    r.g0 = min(warp * share, n4);
+    r.g1 = min(r.g0 + share, n4);
+    const float top = logit_of((uint32_t)r.of_all(r.gather<1>(key_of(best + 0.f), 0, 0, 1), 0, 1));
     if (!(T > 0.f) || !(top > -INFINITY)) {
-        // greedy; a row with nothing above -inf gives token 0
+        // greedy: the lowest index with the largest logit; a row with nothing above -inf gives token 0
+        u64 at = 0;
+        r.for_each([&](float l, int i) {
+            if (l == top) at = max(at, (u64)(0xFFFFFFFFu - (uint32_t)(c0 + i)));
+        });
+        at = r.of_all(r.gather<1>(at, 0, 0, 1), 0, 1);
         if (r.rank == 0 && tid == 0) {
-            p.tokens[row] = top > -INFINITY ? top_i : 0;
+            p.tokens[row] = at ? (int)(0xFFFFFFFFu - (uint32_t)at) : 0;
             if (p.probs) p.probs[row] = 1.f;
         }
         return;
@@ -501,93 +601,143 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             if (values[pad + i] > FLT_MAX) values[pad + i] = FLT_MAX;
         __syncthreads();
     }
-    r.bins_per = fmaxf(fminf(32.f / T, 3.0e38f), 1.0e-37f);
+    r.bins_per = fmaxf(fminf(64.f / T, 3.0e38f), 1.0e-37f);
+    r.bin_step = 1.f / r.bins_per;
 
     // ---- the shortest prefix that the filters keep
     Place place = {0u, 0x7fffffff};                     // everything
-    bool by_k = top_k > 0 && top_k < p.vocab;
     const bool by_p = top_p < 1.f;
-    u64 before = 0;
+    bool by_k = top_k > 0 && top_k < p.vocab, filtered = false;
     if (by_k || by_p) {
         // (the last bin has no end: most of a peaked row is there, and all at one counter would wait for one another)
-        u64 kept = 0;                   // weights
+        const bool weigh = !by_k;       // (with top-k it is only known later what counts)
+        u64 whole = 0;
         uint32_t in_last = 0;
         r.for_each([&](float l, int) {
             const int b = r.bin_of(l);
             if (b < kBins - 1) atomicAdd(&s.bins[b], 1u);
             else ++in_last;
-            if (by_p) kept += r.weight(l);
+            if (weigh) whole += r.weight(l);
         });
         in_last = __reduce_add_sync(0xffffffffu, in_last);
         if (lane == 0 && in_last) atomicAdd(&s.bins[kBins - 1], in_last);
-        u64 whole = r.of_all(r.gather<1>(kept, 0, 0, 0), 0, 0);
+        whole = r.of_all(r.gather<1>(whole, 0, 0, 0), 0, 0);
         r.share_bins();
+        int b_listed = kBins;
+        u64 before = 0;
         if (by_k) {
             const int b = r.bin_reaching((u64)top_k, before, [](int) { return 1ull; });
-            by_k = b < kBins;           // (fewer logits above -inf than that: no filter)
-            if (by_k) place = r.resolve(b, false, (u64)top_k - before, s.all_bins[b]);
+            if (b < kBins) {            // (otherwise fewer logits above -inf than that: no filter)
+                b_listed = b;
+                r.make_list(r.least_of(b));
+                place = r.resolve(b, false, (u64)top_k - before, s.all_bins[b]);
+                filtered = true;
+            }
         }
         if (by_p) {
             // of the weight that top-k leaves top-p keeps a share
             if (by_k) {
-                kept = 0;
+                whole = 0;
                 r.for_each([&](float l, int i) {
-                    if (place.reaches(key_of(l), c0 + i)) kept += r.weight(l);
+                    if (place.reaches(key_of(l), c0 + i)) whole += r.weight(l);
                 });
-                whole = r.of_all(r.gather<1>(kept, 0, 0, 0), 0, 0);
+                whole = r.of_all(r.gather<1>(whole, 0, 0, 0), 0, 0);
             }
             // the first sum that is not below top_p * whole; at least the first token
             const u64 need = min(whole, max((u64)1, (u64)ceil(fmax((double)top_p, 0.0) * (double)whole)));
-            u64 total = 0;
-            int b = r.bin_reaching(need, before, [&](int k) { return r.bin_weight(k); });
-            b = r.settle(b, need, before, total, [&](float l) { return r.bin_of(l); });
-            const Place q = r.resolve(b, true, need - before, total);
-            if (!by_k || q.key > place.key || (q.key == place.key && q.index < place.index)) place = q;
+            int b = min(r.bin_reaching(need, before, [&](int k) { return r.bin_weight(k); }), kBins - 1);
+            const int b0 = max(b - 1, 0), b1 = min(b + 1, kBins - 1);
+            if (!filtered) {
+                b_listed = b1;
+                r.make_list(r.least_of(b1));
+            }
+            // the tokens of the bin and of those beside it, ranked by exact sums; what the bins' middles were too far off for (or
+            // too many tokens) is settled step by step
+            Place q = place;
+            bool found = false;
+            const u64 near = (u64)s.all_bins[b] + (b0 < b ? s.all_bins[b0] : 0) + (b1 > b ? s.all_bins[b1] : 0);
+            if (near <= kCandidates && b1 <= b_listed) {
+                u64 above = 0;
+                r.for_each([&](float l, int i) {
+                    const int bb = r.bin_of(l);
+                    if (bb > b1) return;
+                    const u64 w = r.weight(l);
+                    if (bb < b0) above += w;
+                    else r.put_candidate(l, i, w);
+                });
+                above = r.of_all(r.gather<1>(above, 0, 0, 0), 0, 0);
+                found = r.rank_candidates((int)near, need > above ? need - above : 0, q);        // (0: none does)
+            }
+            if (!found) {
+                u64 total = 0;
+                b = r.settle(b, b_listed, need, before, total, [&](float l) { return r.bin_of(l); });
+                q = r.resolve(b, true, need - before, total);
+            }
+            if (!filtered || q.key > place.key || (q.key == place.key && q.index < place.index)) place = q;
+            filtered = true;
         }
     }
     uint32_t least_key = 0;
-    if (min_p > 0.f) least_key = key_of(__double2float_ru((double)r.weight.top + (double)T * log(fmin((double)min_p, 1.0))) + 0.f);
+    if (min_p > 0.f) {
+        least_key = key_of(__double2float_ru((double)r.weight.top + (double)T * log(fmin((double)min_p, 1.0))) + 0.f);
+        if (!filtered) r.make_list(logit_of(least_key));
+        filtered = true;
+    }
 
-    // ---- running sums in index order: a thread's tokens are neighbours, an odd number of groups of four (no two threads of
-    // a quarter warp then meet on a bank)
-    const int each = ((groups * kVec / 4 + kThreads - 1) / kThreads) | 1;
-    const float4 *g4 = reinterpret_cast<const float4 *>(values);
-    const int g_end = min((tid + 1) * each, (pad + r.n + 3) / 4);
+    // ---- running sums in index order: of the CTAs, of the warps, and within the warp that has the token
     auto kept_weight = [&](float l, int i) -> u64 {
+        if (!filtered) return r.weight(l);
         const uint32_t k = key_of(l);
         return l > -INFINITY && k >= least_key && place.reaches(k, c0 + i) ? r.weight(l) : 0;
     };
     u64 mine = 0;
-    for (int g = tid * each; g < g_end; ++g) {
-        const float4 x = g4[g];
-        const int i = g * 4 - pad;
-        mine += kept_weight(x.x, i) + kept_weight(x.y, i + 1) + kept_weight(x.z, i + 2) + kept_weight(x.w, i + 3);
-    }
+    r.for_each([&](float l, int i) { mine += kept_weight(l, i); });
     const int slot = r.gather<1>(mine, 0, 0, 0);
     const u64 total = r.of_all(slot, 0, 0);
     u64 at = 0;
     for (int k = 0; k < r.rank; ++k) at += s.box[slot][k][0];
     // the token's running sum is the first above u * total
     const u64 goal = (u64)((double)u * (double)total);
-    if (goal < at || goal >= at + s.box[slot][r.rank][0]) return;
-    u64 in = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const u64 y = __shfl_up_sync(0xffffffffu, in, o);
-        if (lane >= o) in += y;
-    }
-    for (int w = 0; w < warp; ++w) at += s.warp_val[0][w];
-    at += in - mine;
-    if (goal >= at && goal < at + mine) {
-        for (int i = tid * each * 4 - pad; i < g_end * 4 - pad; ++i) {
-            const u64 w = kept_weight(r.v[i], i);
-            if (goal < at + w) {
-                p.tokens[row] = c0 + i;
-                if (p.probs) p.probs[row] = (float)((double)w / (double)total);
-                break;
+    for (int w = 0; w < kWarps; ++w) at += w < warp ? s.warp_val[0][w] : 0;
+    if (goal < at || goal >= at + s.warp_val[0][warp]) return;
+    const int step = r.listed >= 0 ? 32 : 128;
+    for (int e = r.listed >= 0 ? 0 : r.g0 * 4; e < (r.listed >= 0 ? r.listed : r.g1 * 4); e += step) {
+        // a lane's tokens: one of the list, or four neighbours
+        int i = -pad;
+        u64 w[4] = {0, 0, 0, 0};
+        if (r.listed >= 0) {
+            if (e + lane < r.listed) {
+                i = s.list[warp][e + lane];
+                w[0] = kept_weight(r.v[i], i);
             }
-            at += w;
+        } else if (e + 4 * lane < r.g1 * 4) {
+            i = e + 4 * lane - pad;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (r.v[i + k] > -INFINITY) w[k] = kept_weight(r.v[i + k], i + k);
         }
+        const u64 own = (w[0] + w[1]) + (w[2] + w[3]);
+        u64 in = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 y = __shfl_up_sync(0xffffffffu, in, o);
+            if (lane >= o) in += y;
+        }
+        u64 from_here = at + in - own;
+        at += __shfl_sync(0xffffffffu, in, 31);
+        if (goal >= at) continue;
+        if (goal >= from_here && goal < from_here + own) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (goal >= from_here && goal < from_here + w[k]) {
+                    p.tokens[row] = c0 + i + k;
+                    if (p.probs) p.probs[row] = (float)((double)w[k] / (double)total);
+                }
+                from_here += w[k];
+            }
+        }
+        return;
     }
 }
 
