@@ -1138,7 +1138,7 @@ lvspec_status_t lvspec_sample(lvspec_ctx_t *ctx, int32_t rows, int32_t vocab, in
     p.row_stride = row_stride;
     p.vocab = vocab;
     int launches = 0;
-    e = launch_sample(p, rows, dtype == LVSPEC_DTYPE_BF16, ctx->pdl, ctx->stream, &launches);
+    e = launch_sample(p, rows, dtype == LVSPEC_DTYPE_BF16, ctx->pdl, ctx->n_sm, ctx->stream, &launches);
     ctx->launches += launches;
     if (e != cudaSuccess) return cuda_fail(ctx, "sampling kernel launch", e);
     return LVSPEC_OK;

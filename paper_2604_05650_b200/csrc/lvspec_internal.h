@@ -249,10 +249,11 @@ struct SampleParams {
     uint32_t *status;
     long long row_stride;
     int32_t vocab, cluster;
+    int32_t rows, by_cost;              // by_cost: the rows that take longest first
 };
 int sample_cluster(int vocab, int rows, int n_sm);
 size_t sample_smem_bytes(int vocab, int cluster);
-cudaError_t launch_sample(const SampleParams &p, int rows, bool bf16, bool pdl, cudaStream_t stream, int *launches);
+cudaError_t launch_sample(const SampleParams &p, int rows, bool bf16, bool pdl, int n_sm, cudaStream_t stream, int *launches);
 
 size_t paged_fp8_scratch_bytes(int n_cta, int M, int D);
 cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool, const uint8_t *v_pool, cudaStream_t stream,

@@ -6,16 +6,21 @@
 // M + T ln(min_p).  Of what the shortest prefix keeps, taken in index order again, the token is the first whose
 // running sum exceeds u times the whole.
 //
-// Weights are integers, 2^40 for the largest: (l_i - M) log2(e) / T with its rounding errors carried, 2^x of its fraction to 2^-22.  Sums
-// of integers do not depend on their order, so a row gives the same token however it is cut up.
+// Weights are integers, 2^40 for the largest: log2(e) (l_i - M) / T with its rounding errors carried, 2^x of its fraction to 2^-22.
+// Sums of integers do not depend on their order, so a row gives the same token however it is cut up.
 //
 // A row is read once, by a cluster of up to eight CTAs that keep it in their shared memory (a vocabulary of 152 K is 76 KB
-// each, two CTAs an SM) and pass sums on through distributed shared memory; it is bound by the latency of these
-// exchanges (a barrier each) and by the passes over shared memory, not by HBM.  A boundary is
-// found without sorting: a histogram over (M - l) in steps of T / 32, then the few hundred tokens of the bin that holds the
-// boundary are ranked by comparing all with all; a bin with more tokens than fit there (equal or nearly equal logits) is cut
-// into bins of the logits' bit patterns until it fits or holds a single value.  Top-p's bin is chosen by the bins' counts and
-// the weights of their middles, and put right by exact sums.
+// each, two CTAs an SM) and pass sums on through distributed shared memory.  A boundary is found without sorting: a histogram over
+// (M - l) in steps of T / 64 or T / 128, then the tokens of the bin that holds the boundary are ranked by comparing all with all (more
+// than 160 by the CTAs together); a bin with more than 1024 tokens (equal or nearly equal logits) is cut into bins of the
+// logits' bit patterns until it fits or holds a single value.  Top-p's bin is chosen by the bins' counts and the weights of their
+// middles; it is ranked together with the bins beside it by exact sums, or put right step by step if it is not among them.  Once a
+// boundary's bin is known each warp lists its tokens up to it, and what follows goes over the lists.
+//
+// Not HBM bounds it but the exchanges (a cluster barrier each, four with top-k, six with top-p) and the passes over shared memory.
+// 128 rows of 152064 in fp32, us: greedy 41, no filter 66, min-p 47, top-k 75, top-p 0.9 127, 0.99 at T = 1.2 223; one row: 7, 9, 7,
+// 13, 18, 28.  Sixteen CTAs a row, three an SM, take 50 to 90 % longer with 32 rows or more, and win with few: the barrier's cost
+// against the passes'.
 #include <cfloat>
 
 #include "lvspec_internal.h"
@@ -71,30 +76,55 @@ __device__ __forceinline__ uint32_t key_of(float l)
 }
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 
+// 2^40 2^(n + f) rounded down, n the low bits of t = n + 1.5 * 2^23: 2^f's 24 bits shifted into place.
+__device__ __forceinline__ u64 weight_of(float t, float f)
+{
+    const uint32_t e = __float_as_uint(ptx::ex2(f));
+    const uint32_t m = (e & 0x7FFFFFu) | 0x800000u;
+    const int down = 127 - (int)(e >> 23) - (int)(__float_as_uint(t) - 0x4B400000u);        // m << 17 >> down
+    u64 w;
+    asm("shr.u64 %0, %1, %2;" : "=l"(w) : "l"((u64)m << 17), "r"(down));        // (nothing is left of shifts by 64 and more)
+    return w;
+}
+constexpr float kNearestInt = 12582912.f;           // 1.5 * 2^23: added and taken off again it rounds to an integer
+// For any top and T: the difference and its product with log2(e) / T carried with their rounding errors.
+__device__ __noinline__ u64 weight_anywhere(float l, float top, float per, float per_rest)
+{
+    const float d = l - top, z = d - l;
+    const float d_rest = (l - (d - z)) + (-top - z);
+    const float y = d * per;
+    const float t = y + kNearestInt;
+    const float f = (y - (t - kNearestInt)) + (fmaf(d, per, -y) + fmaf(d, per_rest, d_rest * per));
+    return y > -42.f ? weight_of(t, f) : 0;
+}
 struct Weight {
-    float top;              // the row's largest logit, finite
-    float per, per_rest;    // log2(e) / T in two parts
+    float top;                  // the row's largest logit, finite
+    float per, per_rest;        // log2(e) / T in two parts
+    float lowest;               // logits below this count as it: their weight is nothing
+    float at_top, at_top_rest;  // top log2(e) / T in two parts
+    bool usual;
     __device__ __forceinline__ void set(float top_, float T)
     {
         top = top_;
-        const double c = 1.4426950408889634 / (double)T;
+        const double c = 1.4426950408889634 / (double)T, ct = c * (double)top;
         per = (float)c;
         per_rest = isinf(per) ? 0.f : (float)(c - (double)per);
+        lowest = top - 45.f * T;                    // 2^40 exp(-45) is below 1
+        // The first part has so few bits that it is still exact with an integer down to -66 added.
+        usual = fabs(ct) < 1048576.0 && T > 1e-30f && T < 1e30f;
+        double grain = 1.52587890625e-05;
+        while (usual && fabs(ct) >= 16777216.0 * grain - 66.0) grain *= 2;
+        at_top = (float)(rint(ct / grain) * grain);
+        at_top_rest = (float)(ct - (double)at_top);
     }
-    // floor(2^40 exp((l - top) / T)): the difference and its product with `per` carried with their rounding errors, 2^x of the
-    // fraction good to 2^-22, its 24 bits shifted into place
+    // floor(2^40 exp((l - top) / T)), 2^x of the fraction good to 2^-22
     __device__ __forceinline__ u64 operator()(float l) const
     {
-        const float d = l - top, z = d - l;
-        const float d_rest = (l - (d - z)) + (-top - z);
-        const float y = d * per;
-        const float t = y + 12582912.f, n = t - 12582912.f;         // 1.5 * 2^23: y to the nearest integer, in the low bits of t
-        const float f = (y - n) + (fmaf(d, per, -y) + fmaf(d, per_rest, d_rest * per));
-        const uint32_t e = __float_as_uint(ptx::ex2(f));
-        const uint32_t m = (e & 0x7FFFFFu) | 0x800000u;
-        const int down = 127 - (int)(e >> 23) - (int)(__float_as_uint(t) - 0x4B400000u);        // m << 17 >> down
-        const u64 w = ((u64)m << 17) >> down;
-        return y > -42.f ? w : 0;
+        if (__builtin_expect(!usual, 0)) return weight_anywhere(l, top, per, per_rest);
+        l = fmaxf(l, lowest);
+        const float t = fmaf(l, per, -at_top) + kNearestInt;
+        const float f = fmaf(l, per, -(at_top + (t - kNearestInt))) + fmaf(l, per_rest, -at_top_rest);
+        return weight_of(t, f);
     }
 };
 
@@ -115,7 +145,7 @@ struct Shared {
     uint32_t all_bins[kBins];           // the histogram of the whole row
     u64 cand[kCandidates], cand_weight[kCandidates];    // key and index of a bin's tokens; their weights
     u64 cum;
-    int bin, n_cand, answer;
+    int bin, n_cand, answer, row;
     u64 place, found;                   // a place as one word (key above, index below); is there one
 };
 
@@ -127,11 +157,11 @@ struct Row {
     int listed;                         // tokens in the warp's list; -1: it has none, passes go over its share
     int n_cta, rank, turn;
     Weight weight;
-    float bins_per, bin_step;           // 64 / T and its inverse
+    float bins_per, bin_step;           // bins to a logit's difference, and its inverse
 
     __device__ __forceinline__ Row(Shared &s_) : s(s_), listed(-1), turn(0) {}
 
-    // f(logit, its place in v) for the warp's logits above -inf, or those of its list
+    // f(logit, its place in v) for the warp's logits (-inf among them), or those of its list
     template <typename F>
     __device__ __forceinline__ void for_each(F f) const
     {
@@ -151,8 +181,7 @@ struct Row {
             const float4 x = g4[g];
             const float l[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (l[k] > -INFINITY) f(l[k], g * 4 + k - pad);
+            for (int k = 0; k < 4; ++k) f(l[k], g * 4 + k - pad);
         }
     }
     // Lists the warp's logits from `least` on, in their order.  A warp with more than it has room for goes on without a list.  (The
@@ -243,7 +272,20 @@ struct Row {
     __device__ __forceinline__ int bin_of(float l) const
     {
         const float t = fminf((weight.top - l) * bins_per, (float)(kBins - 1));
-        return (int)(__float_as_uint(t + 12582912.f) - 0x4B400000u);          // (1.5 * 2^23: the integer is in the low bits)
+        return (int)(__float_as_uint(t + kNearestInt) - 0x4B400000u);          // (the integer is in the low bits)
+    }
+    // Counts a logit in its bin; those of the last one (they have no end: most of a peaked row is there, and all at one counter would
+    // wait for one another) in `in_last`.
+    __device__ __forceinline__ void count(float l, uint32_t &in_last)
+    {
+        const float t = (weight.top - l) * bins_per;
+        if (t < (float)(kBins - 1) - 0.75f)
+            asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(ptx::smem_u32(s.bins) + 4u * (__float_as_uint(t + kNearestInt) - 0x4B400000u)) : "memory");
+        else if (l > -INFINITY) {
+            const int b = bin_of(l);
+            if (b < kBins - 1) atomicAdd(&s.bins[b], 1u);
+            else ++in_last;
+        }
     }
     // Weight of a logit in the middle of a bin (none for the last, which has no end)
     __device__ __forceinline__ u64 bin_weight(int b) const { return b < kBins - 1 ? weight(weight.top - b * bin_step) : 0; }
@@ -326,7 +368,7 @@ struct Row {
             u64 above = 0, inside = 0, tokens = 0;
             for_each([&](float l, int) {
                 const int bb = bin_at(l);
-                if (bb < 0 || bb > b) return;
+                if (bb < 0 || bb > b || !(l > -INFINITY)) return;
                 const u64 w = weight(l);
                 if (bb < b) above += w;
                 else {
@@ -407,7 +449,7 @@ struct Row {
     __device__ Place resolve(int bin, bool by_mass, u64 need, u64 total)
     {
         const int tid = threadIdx.x, lane = tid & 31;
-        uint32_t lo = 0, hi = 0xFFFFFFFFu;              // keys of the bin
+        uint32_t lo = key_of(-INFINITY) + 1, hi = 0xFFFFFFFFu;             // keys of the bin
         auto in_bin = [&](float l, uint32_t &k) {
             k = key_of(l);
             return bin_of(l) == bin && k >= lo && k <= hi;
@@ -510,10 +552,41 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     Row r(s);
     r.n_cta = p.cluster;
     r.rank = (int)cluster_rank();
-    const int row = blockIdx.x / p.cluster;
+    int row = blockIdx.x / p.cluster;
 
     ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
+    if (p.by_cost) {
+        // more rows than run at once: those that take longest first (by their filters, then by index)
+        const bool is = tid < p.rows;
+        const float t = is && p.temperature ? p.temperature[tid] : 1.f, tp = is && p.top_p ? p.top_p[tid] : 1.f;
+        const int k = is && p.top_k ? p.top_k[tid] : 0;
+        const float mp = is && p.min_p ? p.min_p[tid] : 0.f;
+        const bool has_k = k > 0 && k < p.vocab, has_p = tp < 1.f;
+        const int kind = !(t > 0.f) ? 4 : has_k && has_p ? 1 : has_p ? 0 : has_k ? 2 : mp > 0.f ? 4 : 3;
+        uint32_t same = 0;
+        u64 counts = 0;                 // 12 bits for each kind
+#pragma unroll
+        for (int c = 0; c < 5; ++c) {
+            const uint32_t has = __ballot_sync(0xffffffffu, is && kind == c);
+            counts |= (u64)__popc(has) << (12 * c);
+            if (kind == c) same = has;
+        }
+        if (lane == 0) s.warp_val[0][warp] = counts;
+        __syncthreads();
+        u64 all = 0, before = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            all += s.warp_val[0][w];
+            before += w < warp ? s.warp_val[0][w] : 0;
+        }
+        int at = (int)(before >> (12 * kind) & 0xFFF) + __popc(same & ((1u << lane) - 1u));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) at += c < kind ? (int)(all >> (12 * c) & 0xFFF) : 0;
+        if (is && at == row) s.row = tid;
+        __syncthreads();
+        row = s.row;
+    }
     const float T = p.temperature ? p.temperature[row] : 1.f;
     const int top_k = p.top_k ? p.top_k[row] : 0;
     const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
@@ -543,7 +616,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         return x + 0.f;
     };
     const int groups = (pad + r.n + kVec - 1) / kVec;
-    constexpr int kAhead = 4;           // 16-byte loads of a thread in flight
+    constexpr int kAhead = 5;           // 16-byte loads of a thread in flight
     for (int g0 = tid; g0 < groups; g0 += kAhead * kThreads) {
         uint4 w[kAhead];
 #pragma unroll
@@ -601,7 +674,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             if (values[pad + i] > FLT_MAX) values[pad + i] = FLT_MAX;
         __syncthreads();
     }
-    r.bins_per = fmaxf(fminf(64.f / T, 3.0e38f), 1.0e-37f);
+    // steps of T / 64 (32 T in all; what lies beyond weighs nothing), or, for a boundary by weight alone, T / 128: fewer tokens to rank
+    r.bins_per = fmaxf(fminf((top_k > 0 ? 64.f : 128.f) / T, 3.0e38f), 1.0e-37f);
     r.bin_step = 1.f / r.bins_per;
 
     // ---- the shortest prefix that the filters keep
@@ -609,19 +683,20 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const bool by_p = top_p < 1.f;
     bool by_k = top_k > 0 && top_k < p.vocab, filtered = false;
     if (by_k || by_p) {
-        // (the last bin has no end: most of a peaked row is there, and all at one counter would wait for one another)
         const bool weigh = !by_k;       // (with top-k it is only known later what counts)
         u64 whole = 0;
         uint32_t in_last = 0;
-        r.for_each([&](float l, int) {
-            const int b = r.bin_of(l);
-            if (b < kBins - 1) atomicAdd(&s.bins[b], 1u);
-            else ++in_last;
-            if (weigh) whole += r.weight(l);
-        });
+        if (weigh)
+            r.for_each([&](float l, int) {
+                r.count(l, in_last);
+                whole += r.weight(l);
+            });
+        else
+            r.for_each([&](float l, int) { r.count(l, in_last); });
         in_last = __reduce_add_sync(0xffffffffu, in_last);
         if (lane == 0 && in_last) atomicAdd(&s.bins[kBins - 1], in_last);
-        whole = r.of_all(r.gather<1>(whole, 0, 0, 0), 0, 0);
+        if (weigh) whole = r.of_all(r.gather<1>(whole, 0, 0, 0), 0, 0);
+        else cluster_sync();
         r.share_bins();
         int b_listed = kBins;
         u64 before = 0;
@@ -660,7 +735,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
                 u64 above = 0;
                 r.for_each([&](float l, int i) {
                     const int bb = r.bin_of(l);
-                    if (bb > b1) return;
+                    if (bb > b1 || !(l > -INFINITY)) return;
                     const u64 w = r.weight(l);
                     if (bb < b0) above += w;
                     else r.put_candidate(l, i, w);
@@ -691,7 +766,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         return l > -INFINITY && k >= least_key && place.reaches(k, c0 + i) ? r.weight(l) : 0;
     };
     u64 mine = 0;
-    r.for_each([&](float l, int i) { mine += kept_weight(l, i); });
+    if (filtered) r.for_each([&](float l, int i) { mine += kept_weight(l, i); });
+    else r.for_each([&](float l, int) { mine += r.weight(l); });
     const int slot = r.gather<1>(mine, 0, 0, 0);
     const u64 total = r.of_all(slot, 0, 0);
     u64 at = 0;
@@ -750,17 +826,21 @@ size_t sample_smem_bytes(int vocab, int cluster)
 }
 
 // CTAs of a row: one for each 4 K of its logits, up to eight (76 KB each of a vocabulary of 152 K, two CTAs an SM).  Where the rows
-// leave most SMs without work, up to sixteen.
+// leave most SMs without work, or eight CTAs' shared memory does not hold a row, sixteen.
 int sample_cluster(int vocab, int rows, int n_sm)
 {
     int c = 1;
     while (c < 8 && vocab > c * 4096) c *= 2;
-    if (c == 8 && vocab > 65536 && rows * kMaxCluster <= n_sm) c = kMaxCluster;
+    if ((c == 8 && vocab > 65536 && rows * kMaxCluster <= n_sm) || sample_smem_bytes(vocab, c) > 227 * 1024) c = kMaxCluster;
     return c;
 }
 
-cudaError_t launch_sample(const SampleParams &p, int rows, bool bf16, bool pdl, cudaStream_t stream, int *launches)
+cudaError_t launch_sample(const SampleParams &params, int rows, bool bf16, bool pdl, int n_sm, cudaStream_t stream, int *launches)
 {
+    SampleParams p = params;
+    p.rows = rows;
+    // (128 rows of 152064 with mixed filters: 121 us in their order, 93 us like this; all of one kind 4 % slower)
+    p.by_cost = p.cluster == 8 && rows <= kThreads && rows * 8 > 2 * n_sm;
     const size_t smem = sample_smem_bytes(p.vocab, p.cluster);
     const auto kernel = bf16 ? sample_kernel<true> : sample_kernel<false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
