@@ -1320,7 +1320,7 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
     const int n8 = p.M > 96 ? (p.M + 15) / 16 * 2 : (p.M + 7) / 8;      // chunks of eight columns
     P.NP = (n8 + 1) / 2 * 16;
     // as many streams as tensor memory holds accumulators for, beside 2 x 64 columns of V^T and the S^T buffers
-    const int streams = P.NP <= 32 ? 4 : P.NP <= 48 ? 3 : P.NP <= 96 ? 2 : 1;
+    const int streams = P.NP <= 96 ? 2 : 1;
     const int s_log2 = kVBufs * 64 + (streams + 4) * P.NP <= 512 ? 2 : 1, p_log2 = P.NP <= 96 ? 2 : 1;
     int cols = 32;
     while (cols < kVBufs * 64 + (streams + (1 << s_log2)) * P.NP) cols *= 2;
@@ -1334,12 +1334,12 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
     if (!make_pool_map(&tk, k_pool, p) || !make_pool_map(&tv, v_pool, p)) return cudaErrorInvalidValue;
     cudaError_t e;
     switch (n8) {
-        case 1: e = launch_attention<4, 4, 1>(P, tk, tv, stream, launches); break;
-        case 2: e = launch_attention<4, 4, 2>(P, tk, tv, stream, launches); break;
-        case 3: e = launch_attention<4, 4, 3>(P, tk, tv, stream, launches); break;
-        case 4: e = launch_attention<4, 4, 4>(P, tk, tv, stream, launches); break;
-        case 5: e = launch_attention<3, 3, 5>(P, tk, tv, stream, launches); break;
-        case 6: e = launch_attention<3, 3, 6>(P, tk, tv, stream, launches); break;
+        case 1: e = launch_attention<2, 2, 1>(P, tk, tv, stream, launches); break;
+        case 2: e = launch_attention<2, 2, 2>(P, tk, tv, stream, launches); break;
+        case 3: e = launch_attention<2, 2, 3>(P, tk, tv, stream, launches); break;
+        case 4: e = launch_attention<2, 2, 4>(P, tk, tv, stream, launches); break;
+        case 5: e = launch_attention<2, 2, 5>(P, tk, tv, stream, launches); break;
+        case 6: e = launch_attention<2, 2, 6>(P, tk, tv, stream, launches); break;
         case 7: e = launch_attention<2, 2, 7>(P, tk, tv, stream, launches); break;
         case 8: e = launch_attention<2, 2, 8>(P, tk, tv, stream, launches); break;
         case 9: e = launch_attention<2, 2, 9>(P, tk, tv, stream, launches); break;
