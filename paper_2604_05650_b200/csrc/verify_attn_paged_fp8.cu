@@ -21,16 +21,26 @@
 // where the product takes its A operand.  That keeps the 32 KB of fp16 out of shared memory, whose bandwidth is
 // the next bound after HBM: per tile 16 + 32 KB for K (written, read for either term of q), 16 + 16 for V.
 //
-// The reference exponent of a row is the score of its segment's first position, 2^3 below it; it moves
-// (a tile's maximum over the lanes, accumulators rescaled) when a score passes 2^14.  fp16 then holds a
-// probability with eleven bits down to 2^17 below the first position's, and down to 2^27 with fewer.  V scales are
-// taken relative to 2^(k0): four times the power of two below the segment's first one, moved with the reference.
+// The tiles of a segment (a CTA's share of one sequence and head) go to two streams in turn, each with its own softmax group of
+// four warps, references, sums and accumulators of O, put together when the segment ends: while one group works on a tile the
+// other's products run.  From 97 rows on tensor memory holds one stream, whose two groups share out the columns.  A tile's chain is
+// wait for S^T, pass, vote, P^T there, next K.Q^T: 3700 cycles at 80 rows, 2050 of them the pass (the special-function unit needs
+// 640), and that chain, not HBM, bounds all but the longest launches of few rows.
+//
+// The reference exponent of a row is taken from the stream's first tile: its largest probability there becomes 2^6.  It moves (the
+// tile's pass is taken back, a maximum over the lanes, accumulators rescaled, the pass made again) when a score passes 2^14.  fp16 then
+// holds a probability with eleven bits down to 2^-20 of the first tile's largest, and down to 2^-30 with fewer.  V scales are
+// taken relative to 2^(k0): four times the power of two below the largest of that tile, moved with the references.
 //
 // Work is laid out on the device, from the lengths: the tiles of all (sequence, KV head) pairs in a row are cut into
 // equal shares, one per SM, either at multiples of the share within each pair (no CTA has two pairs) or straight
 // through (a CTA may end one pair and begin the next).  A captured launch so follows lengths that change, and a batch of
 // different lengths keeps all SMs busy.  Partials of pairs that several CTAs share are merged by a second, small
 // kernel; a pair that one CTA has to itself is finished there.
+//
+// Measured, us a call (merge included): 8 heads x 131071 positions x 2 sequences, 20 rows 99 (537 MB, 5.4 TB/s); 16 sequences of
+// 16000 to 32003, 80 rows 238; 32768 positions, 40 rows 28; 8 x 16384 ragged, 7 rows 27; 333 positions 14 (launches and cold code: a
+// CTA's first product is ready 6 us after its lengths).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -47,25 +57,20 @@ using namespace ptx;
 constexpr int kTilePos = 128;
 constexpr int kVBufs = 2;                   // V^T buffers in tensor memory, and sets of four warps that fill them
 constexpr int kConvertWarp0 = 4, kSoftmaxWarp0 = kConvertWarp0 + 4 * kVBufs;
-__host__ __device__ constexpr int threads_of(int groups) { return 32 * kSoftmaxWarp0 + 128 * groups; }      // groups: softmax groups of four warps
+constexpr int kGroups = 2;                  // softmax groups, of four warps each
+constexpr int kThreads = 32 * kSoftmaxWarp0 + 128 * kGroups;
 // Registers of a thread at launch, and what the softmax warps are given when the others have given up theirs (kIssueRegs for the
 // four warps that issue, kConvertRegs for those that convert).
-constexpr int kIssueRegs = 40, kConvertRegs = 48;
-__host__ __device__ constexpr int launch_regs(int groups) { return groups == 4 ? 72 : groups == 3 ? 80 : 96; }
-__host__ __device__ constexpr int softmax_regs(int groups) { return groups == 4 ? 88 : groups == 3 ? 112 : 168; }
+constexpr int kIssueRegs = 40, kConvertRegs = 48, kLaunchRegs = 96, kSoftmaxRegs = 168;
+static_assert(32 * (kConvertWarp0 * kIssueRegs + 4 * kVBufs * kConvertRegs + 4 * kGroups * kSoftmaxRegs) <= kThreads * kLaunchRegs &&
+                  kThreads * kLaunchRegs <= 65536,
+              "a share of the registers that is not there is waited for without end");
 // chunks of columns that the registers hold beside the sums
-__host__ __device__ constexpr int block_of(int groups, int chunks)
+__host__ __device__ constexpr int block_of(int chunks)
 {
-    const int room = (softmax_regs(groups) - 36) / 8 - chunks;
+    const int room = (kSoftmaxRegs - 36) / 8 - chunks;
     return room >= chunks ? chunks : room >= (chunks + 1) / 2 ? (chunks + 1) / 2 : room >= 2 ? 2 : 1;
 }
-__host__ __device__ constexpr bool pool_holds(int groups)
-{
-    return 32 * (kConvertWarp0 * kIssueRegs + 4 * kVBufs * kConvertRegs + 4 * groups * softmax_regs(groups)) <=
-               threads_of(groups) * launch_regs(groups) &&
-           threads_of(groups) * launch_regs(groups) <= 65536;
-}
-static_assert(pool_holds(2) && pool_holds(3) && pool_holds(4), "a share of the registers that is not there is waited for without end");
 constexpr int kMergeWarps = 8;
 constexpr int kMaxBufs = 4;                 // S^T buffers and P^T buffers, at most
 constexpr float kFirst = 6.f;               // log2 of the largest probability of a stream's first tile
@@ -521,11 +526,10 @@ __device__ __forceinline__ int div_by(int x, int d, uint32_t m)
     return q * d > x ? q - 1 : q;
 }
 
-// kGroups softmax groups take the tiles in turn, kStreams of them, each with its own references, sums and accumulators of O (a
-// stream), put together when the segment ends; the groups of a stream (kGroups / kStreams) share out the columns, kC chunks of
-// eight to a group.
-template <int kStreams, int kGroups, int kC>
-__global__ void __launch_bounds__(threads_of(kGroups), 1)
+// The tiles of a segment go to kStreams streams in turn, each with its own references, sums and accumulators of O, put together when
+// the segment ends; the groups of a stream (kGroups / kStreams) share out the columns, kC chunks of eight to a group.
+template <int kStreams, int kC>
+__global__ void __launch_bounds__(kThreads, 1)
 attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v)
 {
     constexpr int kSoftmaxThreads = 128 * kGroups;
@@ -840,10 +844,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         }
     } else if (warp >= kSoftmaxWarp0) {
         // ------------------------------------------------------------ softmax
-        more_registers<softmax_regs(kGroups)>();
+        more_registers<kSoftmaxRegs>();
         const int grp = (warp - kSoftmaxWarp0) >> 2, bar_id = 1 + grp;
         constexpr int kAll = 1 + kGroups;                       // barrier of all softmax threads
-        constexpr int kBlock = block_of(kGroups, kC);
+        constexpr int kBlock = block_of(kC);
         const int stream = grp / kShare, part = grp % kShare;
         const int wq = warp & 3, row = wq * 32 + lane;          // TMEM lane: position of the tile, channel of the output
         const int stid = tid - 32 * kSoftmaxWarp0, gtid = stid & 127;
@@ -1295,14 +1299,14 @@ bool make_pool_map(CUtensorMap *map, const uint8_t *pool, const PagedFp8Params &
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kStreams, int kGroups, int kC>
+template <int kStreams, int kC>
 cudaError_t launch_attention(const KernelParams &P, const CUtensorMap &tk, const CUtensorMap &tv, cudaStream_t stream, int *launches)
 {
-    const auto kernel = attn_paged_fp8_kernel<kStreams, kGroups, kC>;
+    const auto kernel = attn_paged_fp8_kernel<kStreams, kC>;
     const size_t smem = P.sm.total + 1024;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_after(kernel, dim3((unsigned)P.a.n_cta), threads_of(kGroups), smem, P.a.pdl != 0, stream, launches, P, tk, tv);
+    return launch_after(kernel, dim3((unsigned)P.a.n_cta), kThreads, smem, P.a.pdl != 0, stream, launches, P, tk, tv);
 }
 
 }  // namespace
@@ -1319,9 +1323,13 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
     P.a = p;
     const int n8 = p.M > 96 ? (p.M + 15) / 16 * 2 : (p.M + 7) / 8;      // chunks of eight columns
     P.NP = (n8 + 1) / 2 * 16;
-    // as many streams as tensor memory holds accumulators for, beside 2 x 64 columns of V^T and the S^T buffers
+    // Two streams where tensor memory holds the accumulators of both beside 2 x 64 columns of V^T and two S^T buffers.  (Four streams up
+    // to 32 rows and three up to 48, of a group each, with fewer registers a thread: 16 sequences of 9500 to 32000 positions, 8 heads,
+    // 8 rows 113 us against 112, 32 rows 127 against 118, 40 rows 152 against 141, 48 rows 145 against 141.)
     const int streams = P.NP <= 96 ? 2 : 1;
     const int s_log2 = kVBufs * 64 + (streams + 4) * P.NP <= 512 ? 2 : 1, p_log2 = P.NP <= 96 ? 2 : 1;
+    // (a group's wait for its S^T buffer's next round must find the round before ended)
+    if (streams > 1 << s_log2) return cudaErrorInvalidValue;
     int cols = 32;
     while (cols < kVBufs * 64 + (streams + (1 << s_log2)) * P.NP) cols *= 2;
     P.tmem_cols = cols;
@@ -1334,20 +1342,20 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
     if (!make_pool_map(&tk, k_pool, p) || !make_pool_map(&tv, v_pool, p)) return cudaErrorInvalidValue;
     cudaError_t e;
     switch (n8) {
-        case 1: e = launch_attention<2, 2, 1>(P, tk, tv, stream, launches); break;
-        case 2: e = launch_attention<2, 2, 2>(P, tk, tv, stream, launches); break;
-        case 3: e = launch_attention<2, 2, 3>(P, tk, tv, stream, launches); break;
-        case 4: e = launch_attention<2, 2, 4>(P, tk, tv, stream, launches); break;
-        case 5: e = launch_attention<2, 2, 5>(P, tk, tv, stream, launches); break;
-        case 6: e = launch_attention<2, 2, 6>(P, tk, tv, stream, launches); break;
-        case 7: e = launch_attention<2, 2, 7>(P, tk, tv, stream, launches); break;
-        case 8: e = launch_attention<2, 2, 8>(P, tk, tv, stream, launches); break;
-        case 9: e = launch_attention<2, 2, 9>(P, tk, tv, stream, launches); break;
-        case 10: e = launch_attention<2, 2, 10>(P, tk, tv, stream, launches); break;
-        case 11: e = launch_attention<2, 2, 11>(P, tk, tv, stream, launches); break;
-        case 12: e = launch_attention<2, 2, 12>(P, tk, tv, stream, launches); break;
-        case 14: e = launch_attention<1, 2, 7>(P, tk, tv, stream, launches); break;
-        default: e = launch_attention<1, 2, 8>(P, tk, tv, stream, launches); break;
+        case 1: e = launch_attention<2, 1>(P, tk, tv, stream, launches); break;
+        case 2: e = launch_attention<2, 2>(P, tk, tv, stream, launches); break;
+        case 3: e = launch_attention<2, 3>(P, tk, tv, stream, launches); break;
+        case 4: e = launch_attention<2, 4>(P, tk, tv, stream, launches); break;
+        case 5: e = launch_attention<2, 5>(P, tk, tv, stream, launches); break;
+        case 6: e = launch_attention<2, 6>(P, tk, tv, stream, launches); break;
+        case 7: e = launch_attention<2, 7>(P, tk, tv, stream, launches); break;
+        case 8: e = launch_attention<2, 8>(P, tk, tv, stream, launches); break;
+        case 9: e = launch_attention<2, 9>(P, tk, tv, stream, launches); break;
+        case 10: e = launch_attention<2, 10>(P, tk, tv, stream, launches); break;
+        case 11: e = launch_attention<2, 11>(P, tk, tv, stream, launches); break;
+        case 12: e = launch_attention<2, 12>(P, tk, tv, stream, launches); break;
+        case 14: e = launch_attention<1, 7>(P, tk, tv, stream, launches); break;
+        default: e = launch_attention<1, 8>(P, tk, tv, stream, launches); break;
     }
     if (e != cudaSuccess) return e;
     const int rows = p.B * p.gamma * p.Hq;
