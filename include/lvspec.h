@@ -17,7 +17,9 @@
  * Around them, each documented at its declaration: the attention on a paged
  * cache, with several visual spans, and on a draft-token tree; the acceptance
  * pass with the emit step, with host buffers, and without any allocation; the
- * paper's own relevance score (Eq. 4) as an alternative input to the rule.
+ * paper's own relevance score (Eq. 4) as an alternative input to the rule; a decoding step
+ * on a paged fp8 cache whose lengths live on the device (pages for the new tokens, their K and V
+ * into the cache, the attention that reads it); and sampling from logits.
  *
  * Conventions
  *   - "device" pointers are CUDA global memory of the context's device; "host"
@@ -493,13 +495,14 @@ lvspec_status_t lvspec_append_paged_fp8(lvspec_ctx_t *ctx, int32_t n_tokens, int
  * shape->n_split must be 0: tiles are shared out on the device, from the lengths.  gamma = 1 is
  * plain decoding.  Cache contents at and behind kv_len may be anything.
  * Arithmetic: scores are 8-bit x (q in two E4M3 terms), accumulated in fp32; softmax, its sums and the visual mass are
- * fp32; the product with V is fp16 x fp16 accumulated in fp32, probabilities in fp16 relative to the
- * first position a CTA works on: those below 2^-27 of it, times the ratio of the V scales, vanish from `out`.
- * q loses nothing down to 2^-10 of the largest magnitude among the rows of a KV head.  A NaN code in a draft
+ * fp32; the product with V is fp16 x fp16 accumulated in fp32, a probability in fp16 together with its V scale: beside the largest
+ * probability of the first 128 positions that a group of warps works on, those below 2^-31, times the ratio of
+ * the V scales, vanish from `out` (not from the sums).  q loses nothing down to 2^-10 of the largest finite magnitude among the rows of
+ * a KV head; a query that holds a NaN or an infinity gives NaN, the others are not touched by it.  A NaN code of V in a draft
  * slot reaches all queries of its head, also those that do not see it.
  * Scratch: lvspec_attention_paged_fp8_workspace_bytes (for lvspec_reserve ahead of a capture).
  * Errors: as lvspec_verify_attention, and INVALID_ARG for an n_split that is not 0, a cache description out of range, kv_capacity not
- * a whole number of pages, max_kv_len out of range, batch * n_kv_heads * ceil(max_kv_len / 128) beyond 2^30;
+ * a whole number of pages, max_kv_len outside 1..kv_capacity or beyond 2^30, batch * n_kv_heads * ceil(max_kv_len / 128) beyond 2^30;
  * UNSUPPORTED for LVSPEC_KERNEL_SIMT. */
 lvspec_status_t lvspec_verify_attention_paged_fp8(lvspec_ctx_t *ctx, const lvspec_attn_shape_t *shape,
                                                   const lvspec_paged_fp8_t *cache, int32_t n_branches, int32_t max_kv_len,

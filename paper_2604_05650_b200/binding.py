@@ -69,6 +69,7 @@ class LvspecError(RuntimeError):
 
 
 _lib = None
+_fast = None             # the calls of a decoding loop without ctypes' conversions, where it has been built
 
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
@@ -145,7 +146,20 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             fn.restype = ctypes.c_int
     if path == LIB_PATH:
         _lib = lib
+        _bind_fast(lib)
     return lib
+
+
+def _bind_fast(lib) -> None:
+    global _fast
+    try:
+        from . import _marshal
+    except ImportError:
+        _fast = None
+        return
+    calls = (lib.lvspec_plan_pages, lib.lvspec_append_paged_fp8, lib.lvspec_verify_attention_paged_fp8, lib.lvspec_sample)
+    _marshal.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in calls))
+    _fast = _marshal
 
 
 def _addr(x) -> Optional[int]:
@@ -199,12 +213,14 @@ class Context:
         if st != OK:
             raise LvspecError(st, self._lib.lvspec_last_error(None).decode())
         self._h = h
+        self._handle = h.value
         self._stream = 0
 
     def close(self) -> None:
         if getattr(self, "_h", None):
             self._lib.lvspec_destroy(self._h)
             self._h = None
+            self._handle = None
 
     def __del__(self):  # pragma: no cover
         try:
@@ -341,6 +357,10 @@ class Context:
     def plan_pages(self, batch, page_size, pages_per_seq, n_pages, max_new, kv_len, n_new, pages_held, n_free,
                    free_pages, block_table, new_kv_len, new_pages_held, new_n_free, token_start, slot_map) -> None:
         """All arrays are device int32; new_kv_len, new_pages_held and new_n_free may be their inputs."""
+        if _fast is not None:
+            st = _fast.plan_pages(self._handle, batch, page_size, pages_per_seq, n_pages, max_new, kv_len, n_new, pages_held, n_free,
+                                  free_pages, block_table, new_kv_len, new_pages_held, new_n_free, token_start, slot_map)
+            return self._check(st) if st else None
         self._check(self._lib.lvspec_plan_pages(
             self._h, int(batch), int(page_size), int(pages_per_seq), int(n_pages), int(max_new), _addr(kv_len), _addr(n_new),
             _addr(pages_held), _addr(n_free), _addr(free_pages), _addr(block_table), _addr(new_kv_len),
@@ -350,6 +370,10 @@ class Context:
                          slot_map, k_pool, v_pool, k_scale, v_scale) -> None:
         """k, v: device bf16 rows [n_kv_heads, head_dim] per token, the token strides in elements apart;
         cache: see ``paged_fp8``."""
+        if _fast is not None:
+            st = _fast.append_paged_fp8(self._handle, n_tokens, n_kv_heads, head_dim, cache, k, v, k_token_stride, v_token_stride,
+                                        slot_map, k_pool, v_pool, k_scale, v_scale)
+            return self._check(st) if st else None
         self._check(self._lib.lvspec_append_paged_fp8(
             self._h, int(n_tokens), int(n_kv_heads), int(head_dim), ctypes.byref(cache), _addr(k), _addr(v), int(k_token_stride),
             int(v_token_stride), _addr(slot_map), _addr(k_pool), _addr(v_pool), _addr(k_scale), _addr(v_scale)))
@@ -358,6 +382,11 @@ class Context:
                                    kv_len, visual_span, out, visual_mass, max_kv_len=None, n_branches: int = 1) -> None:
         """kv_len [B] and visual_span [B, 2] are device int32; no sequence is longer than max_kv_len
         (default: the block table's capacity)."""
+        if _fast is not None:
+            st = _fast.verify_attention_paged_fp8(self._handle, shape, cache, n_branches,
+                                                  shape.kv_capacity if max_kv_len is None else max_kv_len, q, k_pool, v_pool, k_scale,
+                                                  v_scale, block_table, kv_len, visual_span, out, visual_mass)
+            return self._check(st) if st else None
         self._check(self._lib.lvspec_verify_attention_paged_fp8(
             self._h, ctypes.byref(shape), ctypes.byref(cache), int(n_branches),
             shape.kv_capacity if max_kv_len is None else int(max_kv_len), _addr(q), _addr(k_pool), _addr(v_pool), _addr(k_scale),
@@ -367,6 +396,10 @@ class Context:
                row_stride=None) -> None:
         """A token per row of logits (device fp32, or bf16); temperature, top_p, min_p (fp32 [rows]) and top_k (int32
         [rows]) may be None; row_stride in elements (default: vocab)."""
+        if _fast is not None:
+            st = _fast.sample(self._handle, rows, vocab, bool(bf16), logits, vocab if row_stride is None else row_stride, temperature,
+                              top_k, top_p, min_p, uniform, tokens, probs)
+            return self._check(st) if st else None
         self._check(self._lib.lvspec_sample(
             self._h, int(rows), int(vocab), int(bool(bf16)), _addr(logits), int(vocab if row_stride is None else row_stride),
             _addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p), _addr(uniform), _addr(tokens), _addr(probs)))

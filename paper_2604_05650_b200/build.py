@@ -1,15 +1,17 @@
-"""Builds liblvspec.so (sm_100a only) next to this file with nvcc."""
+"""Builds liblvspec.so (sm_100a only) next to this file with nvcc, and _marshal.so, by which binding.py calls it, with gcc."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "liblvspec.so")
+MARSHAL, MARSHAL_SRC = os.path.join(_HERE, "_marshal.so"), os.path.join(CSRC, "marshal.c")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared"]
@@ -28,7 +30,22 @@ def is_stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_marshal(force: bool = False) -> None:
+    """The calls' Python side; without Python's headers binding.py goes by ctypes."""
+    include = sysconfig.get_paths()["include"]
+    header = os.path.join(_ROOT, "include", "lvspec.h")
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        return
+    if not force and os.path.exists(MARSHAL) and os.path.getmtime(MARSHAL) >= max(map(os.path.getmtime, (MARSHAL_SRC, header))):
+        return
+    tmp = MARSHAL + f".{os.getpid()}.tmp"
+    subprocess.run(["gcc", "-O2", "-fPIC", "-shared", "-Wall", "-Wextra", "-I", include, "-I", os.path.dirname(header),
+                    "-o", tmp, MARSHAL_SRC], check=True)
+    os.replace(tmp, MARSHAL)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_marshal(force)
     if not force and not is_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

@@ -36,3 +36,34 @@ def test_a_null_context(name):
 def test_a_null_context_needs_no_workspace():
     shape = binding.attn_shape(1, 1, 1, 1, 128, 128)
     assert binding.load_library().lvspec_attention_paged_fp8_workspace_bytes(None, ctypes.byref(shape)) == 0
+
+
+class Tensor:
+    def __init__(self, address):
+        self.address = address
+
+    def data_ptr(self):
+        return self.address
+
+
+def test_arguments_without_ctypes():
+    """The module that converts the arguments, on a null context: every kind of argument, and what it refuses."""
+    import numpy as np
+    from paper_2604_05650_b200 import build
+    build.build_marshal()
+    binding.load_library()
+    fast = binding._fast
+    assert fast is not None
+    for pointer in (None, 0, 1 << 63, Tensor(4096), np.zeros(3, np.int32)):
+        assert fast.plan_pages(None, 1, np.int64(2), True, 4, 5, *[pointer] * 11) == binding.ERR_INVALID_ARG
+        assert fast.sample(0, 1, 2, False, pointer, 4, *[pointer] * 7) == binding.ERR_INVALID_ARG
+    cache, shape = binding.paged_fp8(16, 1, 16), binding.attn_shape(1, 1, 1, 1, 128, 128)
+    assert fast.append_paged_fp8(None, 1, 1, 64, cache, None, None, 1 << 40, 1, *[None] * 5) == binding.ERR_INVALID_ARG
+    assert fast.verify_attention_paged_fp8(None, shape, cache, 1, 1, *[None] * 10) == binding.ERR_INVALID_ARG
+    for error, call in ((TypeError, lambda: fast.plan_pages(None, 1)), (TypeError, lambda: fast.sample(None, 1, 2, None, *[None] * 9)),
+                        (AttributeError, lambda: fast.plan_pages(None, 1, 1, 1, 1, 1, "x", *[None] * 10)),
+                        (OverflowError, lambda: fast.plan_pages(None, 1, 1, 1, 1, 1, -1, *[None] * 10)),
+                        (TypeError, lambda: fast.append_paged_fp8(None, 1, 1, 64, shape, None, None, 1, 1, *[None] * 5)),
+                        (TypeError, lambda: fast.verify_attention_paged_fp8(None, None, cache, 1, 1, *[None] * 10))):
+        with pytest.raises(error):
+            call()
