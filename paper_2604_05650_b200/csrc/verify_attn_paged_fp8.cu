@@ -193,7 +193,7 @@ __device__ __forceinline__ int part_slot(int cta, bool first) { return 2 * cta +
 
 // ---- shared memory --------------------------------------------------------------------
 struct Smem {
-    uint32_t k, v, q, p, nm, tmx, fac, sums, rows, scale, bars, misc, seg, line, total;
+    uint32_t k, v, q, p, nm, tmx, fac, sums, rows, scale, nan, bars, misc, seg, line, total;
     int ks, vs;                             // K and V slots
     int s_log2, p_log2;                     // S^T and P^T buffers
 };
@@ -216,6 +216,7 @@ Smem smem_map(int D, int NP, int streams, int ks, int vs, int s_log2, int p_log2
     s.sums = o; o += streams * 2 * 4 * NP * 4;   // [stream][all, inside the span][warp of the group][NP]
     s.rows = o; o += NP * 4;
     s.scale = o; o += kMaxBufs * 16 * 4;    // [S^T buffer][K, V][block of the tile]
+    s.nan = o; o += kVBufs * 4 * 4 * 4;
     s.bars = o; o += 8 * (2 * ks + 2 * vs + kBarsFixed);
     s.misc = o; o += 128;                   // TMEM address, abort flag, words of the softmax warps and groups
     s.seg = o; o += (sizeof(Segment) + 15) & ~15u;
@@ -474,6 +475,10 @@ __device__ __forceinline__ void softmax8(const uint32_t *raw, References nm, int
         unpack_f32x2(fma_f32x2(s2, e2, pair(l[2 * k], l[2 * k + 1])), l[2 * k], l[2 * k + 1]);
         float a, b;
         unpack_f32x2(mul_f32x2(e2, v2), a, b);
+        if (kMask) {                    // (v2 is NaN where the cache is: a query that does not see the position takes nothing of it)
+            a = x[2 * k] == 0.f ? 0.f : a;
+            b = x[2 * k + 1] == 0.f ? 0.f : b;
+        }
         w[k] = pack_f16x2(a, b);
     }
     *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -544,6 +549,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
     float *sums_s = reinterpret_cast<float *>(gbase + sm.sums);
     float *scale_s = reinterpret_cast<float *>(gbase + sm.scale);
     int *row_s = reinterpret_cast<int *>(gbase + sm.rows);           // output row of each column
+    uint32_t *nan_s = reinterpret_cast<uint32_t *>(gbase + sm.nan);  // [V^T buffer][converting warp][32 positions]: V is NaN there
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(gbase + sm.misc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(gbase + sm.misc + 4);
     volatile uint32_t *wmax_s = reinterpret_cast<volatile uint32_t *>(gbase + sm.misc + 16);
@@ -580,6 +586,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
             mbar_init(bar0 + 8 * i, count);
         }
         if (lane == 0) *abort_flag = 0;
+        nan_s[lane] = 0;                        // (warps without channels never write theirs)
         fence_proxy_async_smem();
         grid_dependency_wait();
         grid_launch_dependents();
@@ -768,6 +775,8 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 if (!ok) break;
                 tc_fence_after();
                 const int live = seg.len - (seg.t0 + j) * kTilePos;      // positions of this tile below the length
+                const int drafts = gamma > 1 ? live - gamma : kTilePos;  // the first that not all queries see
+                uint32_t nan_at[2] = {0, 0};
                 const uint32_t tile = base + sm.v + vr.idx * slot_bytes;
                 // 16 channels x 64 positions a turn
                 const uint32_t from = tile + lane * D, to = tm_v + set * 64 + ((uint32_t)(wq * 32) << 16);
@@ -778,15 +787,30 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                     uint32_t r[2][4], w[16];
 #pragma unroll
                     for (int u = 0; u < 2; ++u) ldmatrix_b8_x2(from + (half * 2 + u) * 32 * D + ((chunk ^ phase) << 4), r[u]);
-                    if (__builtin_expect(live < kTilePos, 0)) {
-                        // what lies behind the sequence is not the cache's: it may be anything, NaN among it
+                    if (__builtin_expect(min(live, drafts) < kTilePos, 0)) {
+                        // What lies behind the sequence is not the cache's: it may be anything, NaN among it.  A NaN in a draft slot must
+                        // not reach the queries that do not see it, and a zero probability times NaN would: it becomes zero here, and the
+                        // softmax is told of the position.
 #pragma unroll
                         for (int u = 0; u < 2; ++u)
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                const int left = live - (half * 64 + u * 32 + (k >> 1) * 16 + (lane & 3) * 4);
-                                if (left < 4) r[u][k] &= left <= 0 ? 0u : 0xFFFFFFFFu >> (8 * (4 - left));
+                                const int at = half * 64 + u * 32 + (k >> 1) * 16 + (lane & 3) * 4;
+                                const int left = max(0, min(4, live - at)), before = max(0, min(4, drafts - at));
+                                r[u][k] &= (uint32_t)((1ull << (8 * left)) - 1ull);
+                                const uint32_t nan = __vcmpeq4(r[u][k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu) & ~(uint32_t)((1ull << (8 * before)) - 1ull);
+                                r[u][k] &= ~nan;
+                                const uint32_t bits = (nan & 1u) | (nan >> 7 & 2u) | (nan >> 14 & 4u) | (nan >> 21 & 8u);
+                                nan_at[u] |= bits << (at & 31);
                             }
+                        if (h & 1) {
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                const uint32_t all = __reduce_or_sync(0xffffffffu, nan_at[u]);
+                                if (lane == 0) nan_s[(set * 4 + wq) * 4 + half * 2 + u] = all;
+                                nan_at[u] = 0;
+                            }
+                        }
                     }
                     // matrix m of a pair holds registers 2 m (row) and 2 m + 1 (row + 8)
 #pragma unroll
@@ -997,12 +1021,23 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                 __syncwarp();
                 tc_fence_after();
                 const float *sc = scale_s + place(n, sm.s_log2) * 16 + (row >> p.block_log2);
-                const float ck = scale * sc[0], vs = sc[8];
+                const float ck = scale * sc[0];
+                float vs = sc[8];
                 const int ve = (int)((__float_as_uint(vs) >> 23) & 0xFFu) - 127;
                 if (__builtin_expect(begins, 0)) {
                     // the first tile's maxima set the references (below)
                     if (gtid < kC * 8) nm[gtid] = 0.f;
                     named_sync(bar_id, 128);
+                }
+                if (__builtin_expect(tail, 0) && gamma > 1) {
+                    // is V NaN in this draft slot?
+                    // The V^T buffer's round must be this tile's or the one before it for the wait to tell them apart: the products of the
+                    // tile that had the buffer before have ended, and the next to have it waits for this tile's.
+                    if (n >= kVBufs) wait(pv_done(n - kVBufs), round_of(n - kVBufs, sm.p_log2), abort_flag);
+                    wait(vt_full(n & (kVBufs - 1)), (uint32_t)(n / kVBufs) & 1u, abort_flag);
+                    __syncwarp();
+                    const uint32_t *at = nan_s + (n & (kVBufs - 1)) * 16 + wq;
+                    if (((at[0] | at[4] | at[8] | at[12]) >> lane) & 1u) vs = __int_as_float(0x7FFFFFFF);
                 }
                 uint8_t *prow = gbase + sm.p + place(n, sm.p_log2) * (NP * 256) + c_lo * 2048 + row * 16;
                 const Seen seen = tail ? seen_by(pos - (L - gamma), G, gamma, p.branch_len) : Seen{0, 0xFFFFFFFFu};

@@ -78,3 +78,46 @@ def test_calls_one_behind_the_other(ctx):
     for (_, _, _, results), want in zip(jobs, alone):
         for got in results:
             assert same(want, got)
+
+
+@pytest.mark.parametrize("gamma,Hq,branches,D,lens", [(4, 8, 1, 128, [700, 131]), (8, 20, 2, 128, [128, 1290]), (16, 16, 1, 64, [300, 16]),
+                                                     (10, 16, 1, 128, [2000, 1030]), (64, 4, 4, 128, [64, 200]), (1, 8, 1, 128, [77, 900])])
+def test_nan_in_draft_slots(ctx, gamma, Hq, branches, D, lens):
+    """A NaN code of K or V in a draft slot: the queries that see the slot give NaN, the others what they give without it."""
+    import torch
+    c = make(gamma * 3 + D, 2, gamma, Hq, 2, D, 64, 64, lens, [[n // 5, n // 2] for n in lens])
+    c["branches"] = branches
+    clean = call(ctx, c)
+    check(c, *clean)
+    for kind in ("v", "k"):
+        for b, slot in ((0, gamma - 1), (1, gamma // 2)):
+            spoiled = {**c, kind: c[kind].copy()}
+            pos = lens[b] - gamma + slot
+            spoiled[kind][c["table"][b, pos // 64], 1, pos % 64, 37] = 0xFF
+            out, mass = call(ctx, spoiled)
+            assert ctx.device_status() == 0
+            bl = gamma // branches
+            for g in range(gamma):
+                sees = slot <= g and slot // bl == g // bl
+                mine, theirs = out[b, g, Hq // 2:], out[b, g, :Hq // 2]
+                assert torch.equal(theirs, clean[0][b, g, :Hq // 2]) and torch.equal(mass[b, g, :Hq // 2], clean[1][b, g, :Hq // 2])
+                if not sees:
+                    assert torch.equal(mine, clean[0][b, g, Hq // 2:]) and torch.equal(mass[b, g, Hq // 2:], clean[1][b, g, Hq // 2:])
+                elif kind == "v" and gamma == 1:
+                    assert torch.isnan(mine[:, 37]).all() and torch.isfinite(mine[:, :37]).all()
+                else:
+                    assert torch.isnan(mine).all()
+                    assert torch.isnan(mass[b, g, Hq // 2:]).all() == (kind == "k")
+            assert torch.equal(out[1 - b], clean[0][1 - b]) and torch.equal(mass[1 - b], clean[1][1 - b])
+
+
+def test_nan_of_v_before_the_drafts_stays_in_its_channel(ctx):
+    import torch
+    c = make(5, 1, 4, 8, 2, 128, 64, 64, [700], [[10, 600]])
+    clean = call(ctx, c)
+    c["v"] = c["v"].copy()
+    c["v"][c["table"][0, 695 // 64], 0, 695 % 64, 37] = 0x7F
+    out, mass = call(ctx, c)
+    keep = [ch for ch in range(128) if ch != 37]
+    assert torch.isnan(out[0, :, :4, 37]).all() and torch.equal(out[0, :, :4, keep], clean[0][0, :, :4, keep])
+    assert torch.equal(out[0, :, 4:], clean[0][0, :, 4:]) and torch.equal(mass, clean[1])
