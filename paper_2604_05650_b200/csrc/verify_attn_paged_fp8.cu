@@ -769,8 +769,11 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
             n += seg.T;
 #pragma unroll 1
             for (; j < seg.T; j += kVBufs) {
-                ok = wait(v_full(vr.idx), vr.parity, abort_flag);
-                ok = wait(vt_free(set), parity ^ 1u, abort_flag) && ok;       // (at once for the first tile)
+                // The buffer first (at once for the set's first tile): once the products of the tile two before have ended, every earlier tile has
+                // been converted, so that the V slot's barrier cannot still be in the round before (with three slots that
+                // round is the other set's, and loads may land in any order).
+                ok = wait(vt_free(set), parity ^ 1u, abort_flag);
+                ok = wait(v_full(vr.idx), vr.parity, abort_flag) && ok;
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
@@ -1372,7 +1375,8 @@ cudaError_t launch_attn_paged_fp8(const PagedFp8Params &p, const uint8_t *k_pool
     // as many slots as shared memory holds, K's one more where the count is odd (its tile is used first)
     int slots = 12;
     do P.sm = smem_map(p.D, P.NP, streams, (slots + 1) / 2, slots / 2, s_log2, p_log2);
-    while (P.sm.total + 1024 > 227 * 1024 && --slots > 2);
+    while (P.sm.total + 1024 > 227 * 1024 && --slots > 4);
+    if (P.sm.total + 1024 > 227 * 1024) return cudaErrorInvalidValue;        // (six at 128 rows)
     CUtensorMap tk, tv;
     if (!make_pool_map(&tk, k_pool, p) || !make_pool_map(&tv, v_pool, p)) return cudaErrorInvalidValue;
     cudaError_t e;
