@@ -145,7 +145,7 @@ struct Shared {
     uint32_t all_bins[kBins];           // the histogram of the whole row
     u64 cand[kCandidates], cand_weight[kCandidates];    // key and index of a bin's tokens; their weights
     u64 cum;
-    int bin, n_cand, answer, row;
+    int bin, around[2], n_cand, answer, row;
     u64 place, found;                   // a place as one word (key above, index below); is there one
 };
 
@@ -315,9 +315,9 @@ struct Row {
         __syncthreads();
     }
     // First bin at which the running sum, of tokens or (`each`: weight of a token of a bin) of weights, reaches `want`; kBins if none
-    // does.  The sum before it.
+    // does.  The sum before it.  s.around: the first bins that reach the sums `low` and `high`.
     template <typename Each>
-    __device__ int bin_reaching(u64 want, u64 &before, Each each)
+    __device__ int bin_reaching(u64 want, u64 &before, Each each, u64 low = 0, u64 high = 0)
     {
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
         constexpr int kEach = kBins / kThreads;
@@ -335,7 +335,7 @@ struct Row {
             if (lane >= o) in += y;
         }
         if (lane == 31) s.warp_val[0][warp] = in;
-        if (tid == 0) s.bin = kBins;
+        if (tid == 0) s.bin = s.around[0] = s.around[1] = kBins;
         __syncthreads();
         u64 at = in - mine;
 #pragma unroll
@@ -346,6 +346,8 @@ struct Row {
                 s.bin = tid * kEach + k;
                 s.cum = at;
             }
+            if (at < low && at + a[k] >= low) s.around[0] = tid * kEach + k;
+            if (at < high && at + a[k] >= high) s.around[1] = tid * kEach + k;
             at += a[k];
         }
         __syncthreads();
@@ -720,17 +722,36 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             }
             // the first sum that is not below top_p * whole; at least the first token
             const u64 need = min(whole, max((u64)1, (u64)ceil(fmax((double)top_p, 0.0) * (double)whole)));
-            int b = min(r.bin_reaching(need, before, [&](int k) { return r.bin_weight(k); }), kBins - 1);
-            const int b0 = max(b - 1, 0), b1 = min(b + 1, kBins - 1);
+            // The bins' middles are off by exp(1 / 128) at most: the boundary is between the bins that reach 1 % less and 1 % more.
+            // Their tokens are ranked by exact sums, or those of the bin and the ones beside it where they are too many; what
+            // is then not among them (or too many again) is settled step by step.
+            int b = min(r.bin_reaching(need, before, [&](int k) { return r.bin_weight(k); }, max((u64)1, need - need / 100), need + need / 64 + 1),
+                        kBins - 1);
+            int b0 = min(s.around[0], b), b1 = min(max(s.around[1], b), kBins - 1);
+            auto tokens_between = [&](int from, int to) {
+                u64 n = 0;
+                for (int k = from + tid; k <= to; k += kThreads) n += s.all_bins[k];
+                n = __reduce_add_sync(0xffffffffu, (uint32_t)n);
+                __syncthreads();
+                if (lane == 0) s.warp_val[1][warp] = n;
+                __syncthreads();
+                n = 0;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) n += s.warp_val[1][w];
+                return n;
+            };
+            u64 near = tokens_between(b0, b1);
+            if (near > kCandidates) {
+                b0 = max(b - 1, 0);
+                b1 = min(b + 1, kBins - 1);
+                near = tokens_between(b0, b1);
+            }
             if (!filtered) {
                 b_listed = b1;
                 r.make_list(r.least_of(b1));
             }
-            // the tokens of the bin and of those beside it, ranked by exact sums; what the bins' middles were too far off for (or
-            // too many tokens) is settled step by step
             Place q = place;
             bool found = false;
-            const u64 near = (u64)s.all_bins[b] + (b0 < b ? s.all_bins[b0] : 0) + (b1 > b ? s.all_bins[b1] : 0);
             if (near <= kCandidates && b1 <= b_listed) {
                 u64 above = 0;
                 r.for_each([&](float l, int i) {
@@ -825,13 +846,14 @@ size_t sample_smem_bytes(int vocab, int cluster)
     return ((sizeof(Shared) + 15) & ~size_t(15)) + ((size_t)per + 16) * sizeof(float);
 }
 
-// CTAs of a row: one for each 4 K of its logits, up to eight (76 KB each of a vocabulary of 152 K, two CTAs an SM).  Few rows, or rows that
-// eight CTAs' shared memory does not hold, get sixteen: 12 rows of 152064 with top-p 0.9 take 24 us instead of 30, 18 rows 38
-// instead of 32 (then most SMs have two CTAs).
+// CTAs of a row.  Many rows: as few as hold it with two CTAs an SM (19 K logits each, 76 KB), up to eight: every exchange costs
+// the same however little a CTA has.  While the rows leave room for more at once: up to one for each 4 K, and of a large vocabulary
+// sixteen: 12 rows of 152064 with top-p 0.9 take 24 us instead of 30, 18 rows 38 instead of 32 (then most SMs have two CTAs).
 int sample_cluster(int vocab, int rows, int n_sm)
 {
     int c = 1;
-    while (c < 8 && vocab > c * 4096) c *= 2;
+    while (c < 8 && vocab > c * 19456) c *= 2;
+    while (c < 8 && vocab > c * 4096 && rows * c <= n_sm) c *= 2;
     if ((c == 8 && vocab > 65536 && 2 * rows * kMaxCluster <= 3 * n_sm) || sample_smem_bytes(vocab, c) > 227 * 1024) c = kMaxCluster;
     return c;
 }
@@ -841,7 +863,7 @@ cudaError_t launch_sample(const SampleParams &params, int rows, bool bf16, bool 
     SampleParams p = params;
     p.rows = rows;
     // (128 rows of 152064 with mixed filters: 121 us in their order, 93 us like this; all of one kind 4 % slower)
-    p.by_cost = p.cluster == 8 && rows <= kThreads && rows * 8 > 2 * n_sm;
+    p.by_cost = rows <= kThreads && rows * p.cluster > 2 * n_sm;
     const size_t smem = sample_smem_bytes(p.vocab, p.cluster);
     const auto kernel = bf16 ? sample_kernel<true> : sample_kernel<false>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
