@@ -18,9 +18,10 @@
 // boundary's bin is known each warp lists its tokens up to it, and what follows goes over the lists.
 //
 // Not HBM bounds it but the exchanges (a cluster barrier each, four with top-k, six with top-p) and the passes over shared memory.
-// 128 rows of 152064 in fp32, us: greedy 41, no filter 66, min-p 47, top-k 75, top-p 0.9 127, 0.99 at T = 1.2 223; one row: 7, 9, 7,
-// 13, 18, 28.  Sixteen CTAs a row, three an SM, take 50 to 90 % longer with 32 rows or more, and win with few: the barrier's cost
-// against the passes'.
+// 128 rows of 152064 in fp32, us: greedy 41, no filter 67, min-p 47, top-k 76, top-p 0.9 145, 0.99 at T = 1.2 248; one row: 6, 9, 8,
+// 13, 22, 38.  With the bins beside the boundary's only, large vocabularies take 10 % less and rows with few tokens a bin, which then
+// settle step by step, three times as long (2 rows of 3422, top-k and top-p: 52 us instead of 17).  Sixteen CTAs a row, three an SM,
+// take 50 to 90 % longer with 32 rows or more, and win with few: the barrier's cost against the passes'.
 #include <cfloat>
 
 #include "lvspec_internal.h"
@@ -145,7 +146,7 @@ struct Shared {
     uint32_t all_bins[kBins];           // the histogram of the whole row
     u64 cand[kCandidates], cand_weight[kCandidates];    // key and index of a bin's tokens; their weights
     u64 cum;
-    int bin, around[2], n_cand, answer, row;
+    int bin, around[4], n_cand, answer, row;
     u64 place, found;                   // a place as one word (key above, index below); is there one
 };
 
@@ -315,9 +316,9 @@ struct Row {
         __syncthreads();
     }
     // First bin at which the running sum, of tokens or (`each`: weight of a token of a bin) of weights, reaches `want`; kBins if none
-    // does.  The sum before it.  s.around: the first bins that reach the sums `low` and `high`.
+    // does.  The sum before it.  s.around: the first bins that reach these sums.
     template <typename Each>
-    __device__ int bin_reaching(u64 want, u64 &before, Each each, u64 low = 0, u64 high = 0)
+    __device__ int bin_reaching(u64 want, u64 &before, Each each, u64 s0 = 0, u64 s1 = 0, u64 s2 = 0, u64 s3 = 0)
     {
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
         constexpr int kEach = kBins / kThreads;
@@ -335,7 +336,7 @@ struct Row {
             if (lane >= o) in += y;
         }
         if (lane == 31) s.warp_val[0][warp] = in;
-        if (tid == 0) s.bin = s.around[0] = s.around[1] = kBins;
+        if (tid < 5) (tid < 4 ? s.around[tid] : s.bin) = kBins;
         __syncthreads();
         u64 at = in - mine;
 #pragma unroll
@@ -346,8 +347,10 @@ struct Row {
                 s.bin = tid * kEach + k;
                 s.cum = at;
             }
-            if (at < low && at + a[k] >= low) s.around[0] = tid * kEach + k;
-            if (at < high && at + a[k] >= high) s.around[1] = tid * kEach + k;
+            if (at < s0 && at + a[k] >= s0) s.around[0] = tid * kEach + k;
+            if (at < s1 && at + a[k] >= s1) s.around[1] = tid * kEach + k;
+            if (at < s2 && at + a[k] >= s2) s.around[2] = tid * kEach + k;
+            if (at < s3 && at + a[k] >= s3) s.around[3] = tid * kEach + k;
             at += a[k];
         }
         __syncthreads();
@@ -723,11 +726,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             // the first sum that is not below top_p * whole; at least the first token
             const u64 need = min(whole, max((u64)1, (u64)ceil(fmax((double)top_p, 0.0) * (double)whole)));
             // The bins' middles are off by exp(1 / 128) at most: the boundary is between the bins that reach 1 % less and 1 % more.
-            // Their tokens are ranked by exact sums, or those of the bin and the ones beside it where they are too many; what
-            // is then not among them (or too many again) is settled step by step.
-            int b = min(r.bin_reaching(need, before, [&](int k) { return r.bin_weight(k); }, max((u64)1, need - need / 100), need + need / 64 + 1),
+            // Their tokens are ranked by exact sums; where they are too many, those within 0.1 % and of the bins beside (errors of
+            // many bins cancel).  What is then not among them (or too many again) is settled step by step.
+            int b = min(r.bin_reaching(need, before, [&](int k) { return r.bin_weight(k); }, max((u64)1, need - need / 100), need + need / 64 + 1,
+                                       max((u64)1, need - need / 1024), need + need / 1024 + 1),
                         kBins - 1);
             int b0 = min(s.around[0], b), b1 = min(max(s.around[1], b), kBins - 1);
+            const int c0_near = min(s.around[2], max(b - 1, 0)), c1_near = min(max(s.around[3], b + 1), kBins - 1);
             auto tokens_between = [&](int from, int to) {
                 u64 n = 0;
                 for (int k = from + tid; k <= to; k += kThreads) n += s.all_bins[k];
@@ -741,9 +746,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
                 return n;
             };
             u64 near = tokens_between(b0, b1);
-            if (near > kCandidates) {
-                b0 = max(b - 1, 0);
-                b1 = min(b + 1, kBins - 1);
+            if (near > kCandidates || near > (u64)(kRankAlone / 4 * r.n_cta + kRankAlone)) {
+                b0 = c0_near;
+                b1 = c1_near;
                 near = tokens_between(b0, b1);
             }
             if (!filtered) {
