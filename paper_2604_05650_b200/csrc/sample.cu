@@ -743,6 +743,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
                 n = 0;
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) n += s.warp_val[1][w];
+                __syncthreads();            // (the next gather writes them)
                 return n;
             };
             u64 near = tokens_between(b0, b1);
