@@ -45,6 +45,10 @@ __device__ __forceinline__ uint32_t cluster_rank()
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+// Shared memory of another CTA may be written once that CTA is known to run: each says so as it starts, and waits for the others
+// ahead of its first store to them.  (Nothing else is handed over by this.)
+__device__ __forceinline__ void cluster_here() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_all_here() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -559,6 +563,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     r.rank = (int)cluster_rank();
     int row = blockIdx.x / p.cluster;
 
+    cluster_here();
     ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
     if (p.by_cost) {
@@ -657,6 +662,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const int n4 = (pad + r.n + 3) / 4, share = (n4 + kWarps - 1) / kWarps;
     r.g0 = min(warp * share, n4);
     r.g1 = min(r.g0 + share, n4);
+    cluster_all_here();
     const float top = logit_of((uint32_t)r.of_all(r.gather<1>(key_of(best + 0.f), 0, 0, 1), 0, 1));
     if (!(T > 0.f) || !(top > -INFINITY)) {
         // greedy: the lowest index with the largest logit; a row with nothing above -inf gives token 0

@@ -15,3 +15,13 @@ def test_words_of_the_warps_are_read_before_they_are_written_again():
     body = re.search(r"auto tokens_between = .*?\n            \};", code(), flags=re.S).group(0)
     last_read = body.rindex("s.warp_val[1][w]")
     assert "__syncthreads();" in body[last_read:body.rindex("return n;")]
+
+
+def test_no_store_to_a_cta_that_may_not_run_yet():
+    """All CTAs of a cluster arrive before they read anything, and wait before the first exchange."""
+    kernel = code()
+    kernel = kernel[kernel.index("sample_kernel(const SampleParams p)"):kernel.index("size_t sample_smem_bytes")]
+    first = min(kernel.index(f) for f in ("gather<", "st_peer(", "put_candidate(", "share_bins(") if f in kernel)
+    assert 0 < kernel.index("cluster_here();") < kernel.index("cluster_all_here();") < first
+    assert kernel.count("cluster_here();") == kernel.count("cluster_all_here();") == 1
+    assert "return" not in kernel[:first].replace("return x + 0.f;", "")        # (all threads get there)
