@@ -147,8 +147,15 @@ struct Shared {
         uint32_t bins[kBins];           // a histogram of this CTA's tokens
         uint16_t list[kWarps][kListed]; // later the places of those that may be kept, each warp's in its order
     };
-    uint32_t all_bins[kBins];           // the histogram of the whole row
-    u64 cand[kCandidates], cand_weight[kCandidates];    // key and index of a bin's tokens; their weights
+    uint32_t all_bins[kBins];           // the histogram of the whole row, for as long as the row is worked on
+    union {
+        struct {
+            u64 cand[kCandidates], cand_weight[kCandidates];    // key and index of a bin's tokens; their weights
+        };
+        struct {
+            uint32_t cut[kBins], all_cut[kBins];                // while a bin has too many: histograms of it, likewise
+        };
+    };
     u64 cum;
     int bin, around[4], n_cand, answer, row;
     u64 place, found;                   // a place as one word (key above, index below); is there one
@@ -296,8 +303,11 @@ struct Row {
     __device__ __forceinline__ u64 bin_weight(int b) const { return b < kBins - 1 ? weight(weight.top - b * bin_step) : 0; }
     // Bins of the whole row from those of the CTAs (which a cluster barrier has seen done): each CTA adds up its share and hands it
     // to all.
+    template <bool kCut>
     __device__ void share_bins()
     {
+        const uint32_t *bins = kCut ? s.cut : s.bins;
+        uint32_t *all_bins = kCut ? s.all_cut : s.all_bins;
         const int per = kBins / n_cta;
         for (int i = threadIdx.x; i < per / 2; i += kThreads) {
             const int bin = rank * per + 2 * i;
@@ -306,22 +316,22 @@ struct Row {
             for (; r + 4 <= n_cta; r += 4) {
                 u64 y[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = ld_peer(peer_address(ptx::smem_u32(&s.bins[bin]), r + j));
+                for (int j = 0; j < 4; ++j) y[j] = ld_peer(peer_address(ptx::smem_u32(&bins[bin]), r + j));
                 c += (y[0] + y[1]) + (y[2] + y[3]);
             }
-            for (; r < n_cta; ++r) c += ld_peer(peer_address(ptx::smem_u32(&s.bins[bin]), r));
-            for (r = 0; r < n_cta; ++r) st_peer(peer_address(ptx::smem_u32(&s.all_bins[bin]), r), c);
+            for (; r < n_cta; ++r) c += ld_peer(peer_address(ptx::smem_u32(&bins[bin]), r));
+            for (r = 0; r < n_cta; ++r) st_peer(peer_address(ptx::smem_u32(&all_bins[bin]), r), c);
         }
         cluster_sync();
     }
-    __device__ void clear_bins()
+    __device__ void clear_bins(uint32_t *bins)
     {
-        for (int i = threadIdx.x; i < kBins; i += kThreads) s.bins[i] = 0;
+        for (int i = threadIdx.x; i < kBins; i += kThreads) bins[i] = 0;
         __syncthreads();
     }
     // First bin at which the running sum, of tokens or (`each`: weight of a token of a bin) of weights, reaches `want`; kBins if none
     // does.  The sum before it.  s.around: the first bins that reach these sums.
-    template <typename Each>
+    template <bool kCut, typename Each>
     __device__ int bin_reaching(u64 want, u64 &before, Each each, u64 s0 = 0, u64 s1 = 0, u64 s2 = 0, u64 s3 = 0)
     {
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -329,7 +339,7 @@ struct Row {
         u64 a[kEach], mine = 0;
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const uint32_t c = s.all_bins[tid * kEach + k];
+            const uint32_t c = (kCut ? s.all_cut : s.all_bins)[tid * kEach + k];
             a[k] = c ? c * each(tid * kEach + k) : 0;
             mine += a[k];
         }
@@ -516,9 +526,7 @@ struct Row {
                 p.index = (int)of_all(slot, 0, 1) - 1;
                 return p;
             }
-            // ---- bins of the keys
-            __syncthreads();
-            listed = -1;
+            // ---- bins of the keys, in the candidates' place: the row's own histogram and the lists are needed again
             int shift = 0;
             while (((k_hi - k_lo) >> shift) >= (uint32_t)kBins) ++shift;
             lo = k_lo;
@@ -527,21 +535,22 @@ struct Row {
                 uint32_t k;
                 return in_bin(l, k) ? (int)((k_hi - k) >> shift) : -1;
             };
-            clear_bins();
+            clear_bins(s.cut);
             for_each([&](float l, int) {
                 const int b = key_bin(l);
-                if (b >= 0) atomicAdd(&s.bins[b], 1u);
+                if (b >= 0) atomicAdd(&s.cut[b], 1u);
             });
             cluster_sync();
-            share_bins();
+            share_bins<true>();
             u64 at = 0;
             int b;
             if (by_mass) {
-                b = bin_reaching(need, at, [&](int k) { return weight(logit_of(k_hi - ((uint32_t)k << shift))); });
+                b = bin_reaching<true>(need, at, [&](int k) { return weight(logit_of(k_hi - ((uint32_t)k << shift))); });
                 b = settle(b, kBins, need, at, total, key_bin);
             } else {
-                b = bin_reaching(need, at, [](int) { return 1ull; });
-                total = s.all_bins[b];
+                b = bin_reaching<true>(need, at, [](int) { return 1ull; });
+                total = s.all_cut[b];
+                cluster_sync();                 // (all have read them: the next candidates go there)
             }
             need -= at;
             const uint32_t top_key = k_hi - ((uint32_t)b << shift);
@@ -658,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     if (nan_seen) atomicOr(p.status, LVSPEC_DEV_NAN_LOGIT);
     if (tid == 0) s.n_cand = 0, s.found = 0;
-    r.clear_bins();
+    r.clear_bins(s.bins);
     const int n4 = (pad + r.n + 3) / 4, share = (n4 + kWarps - 1) / kWarps;
     r.g0 = min(warp * share, n4);
     r.g1 = min(r.g0 + share, n4);
@@ -708,11 +717,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         if (lane == 0 && in_last) atomicAdd(&s.bins[kBins - 1], in_last);
         if (weigh) whole = r.of_all(r.gather<1>(whole, 0, 0, 0), 0, 0);
         else cluster_sync();
-        r.share_bins();
+        r.share_bins<false>();
         int b_listed = kBins;
         u64 before = 0;
         if (by_k) {
-            const int b = r.bin_reaching((u64)top_k, before, [](int) { return 1ull; });
+            const int b = r.bin_reaching<false>((u64)top_k, before, [](int) { return 1ull; });
             if (b < kBins) {            // (otherwise fewer logits above -inf than that: no filter)
                 b_listed = b;
                 r.make_list(r.least_of(b));
@@ -734,8 +743,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             // The bins' middles are off by exp(1 / 128) at most: the boundary is between the bins that reach 1 % less and 1 % more.
             // Their tokens are ranked by exact sums; where they are too many, those within 0.1 % and of the bins beside (errors of
             // many bins cancel).  What is then not among them (or too many again) is settled step by step.
-            int b = min(r.bin_reaching(need, before, [&](int k) { return r.bin_weight(k); }, max((u64)1, need - need / 100), need + need / 64 + 1,
-                                       max((u64)1, need - need / 1024), need + need / 1024 + 1),
+            int b = min(r.bin_reaching<false>(need, before, [&](int k) { return r.bin_weight(k); }, max((u64)1, need - need / 100),
+                                       need + need / 64 + 1, max((u64)1, need - need / 1024), need + need / 1024 + 1),
                         kBins - 1);
             int b0 = min(s.around[0], b), b1 = min(max(s.around[1], b), kBins - 1);
             const int c0_near = min(s.around[2], max(b - 1, 0)), c1_near = min(max(s.around[3], b + 1), kBins - 1);
