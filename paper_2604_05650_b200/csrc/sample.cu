@@ -280,19 +280,21 @@ struct Row {
         }
         return t;
     }
-    // The nearest bin to (top - l) bins_per; it falls as l rises, whatever the rounding.
-    __device__ __forceinline__ int bin_of(float l) const
+    // The nearest bin to (top - l) bins_per; it falls as l rises, whatever the rounding.  Counting and looking for a bin's tokens
+    // have to round alike, so the product and the sum are written as operations that the compiler may not join into one.
+    __device__ __forceinline__ float in_bins(float l) const { return __fmul_rn(weight.top - l, bins_per); }
+    __device__ __forceinline__ int nearest_bin(float t) const
     {
-        const float t = fminf((weight.top - l) * bins_per, (float)(kBins - 1));
-        return (int)(__float_as_uint(t + kNearestInt) - 0x4B400000u);          // (the integer is in the low bits)
+        return (int)(__float_as_uint(__fadd_rn(t, kNearestInt)) - 0x4B400000u);         // (the integer is in the low bits)
     }
+    __device__ __forceinline__ int bin_of(float l) const { return nearest_bin(fminf(in_bins(l), (float)(kBins - 1))); }
     // Counts a logit in its bin; those of the last one (they have no end: most of a peaked row is there, and all at one counter would
     // wait for one another) in `in_last`.
     __device__ __forceinline__ void count(float l, uint32_t &in_last)
     {
-        const float t = (weight.top - l) * bins_per;
+        const float t = in_bins(l);
         if (t < (float)(kBins - 1) - 0.75f)
-            asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(ptx::smem_u32(s.bins) + 4u * (__float_as_uint(t + kNearestInt) - 0x4B400000u)) : "memory");
+            asm volatile("red.shared.add.u32 [%0], 1;" ::"r"(ptx::smem_u32(s.bins) + 4u * (uint32_t)nearest_bin(t)) : "memory");
         else if (l > -INFINITY) {
             const int b = bin_of(l);
             if (b < kBins - 1) atomicAdd(&s.bins[b], 1u);
