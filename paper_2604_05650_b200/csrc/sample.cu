@@ -92,28 +92,28 @@ __device__ __forceinline__ u64 weight_of(float t, float f)
     return w;
 }
 constexpr float kNearestInt = 12582912.f;           // 1.5 * 2^23: added and taken off again it rounds to an integer
-// For any top and T: the difference and its product with log2(e) / T carried with their rounding errors.
-__device__ __noinline__ u64 weight_anywhere(float l, float top, float per, float per_rest)
+// For any top and T, c = log2(e) / T (its two halves): of fp32 numbers neither 1 / T nor the difference passes the range of fp64.
+__device__ __noinline__ u64 weight_anywhere(float l, float top, int c_hi, int c_lo)
 {
-    const float d = l - top, z = d - l;
-    const float d_rest = (l - (d - z)) + (-top - z);
-    const float y = d * per;
-    const float t = y + kNearestInt;
-    const float f = (y - (t - kNearestInt)) + (fmaf(d, per, -y) + fmaf(d, per_rest, d_rest * per));
-    return y > -42.f ? weight_of(t, f) : 0;
+    const double c = __hiloint2double(c_hi, c_lo);
+    if (!(l > -INFINITY)) return 0;             // (nothing even where T is infinite)
+    const double y = ((double)l - (double)top) * c;
+    if (!(y > -42.0)) return 0;
+    const double n = rint(y);
+    return weight_of((float)n + kNearestInt, (float)(y - n));
 }
 struct Weight {
     float top;                  // the row's largest logit, finite
     float per, per_rest;        // log2(e) / T in two parts
     float lowest;               // logits below this count as it: their weight is nothing
-    float at_top, at_top_rest;  // top log2(e) / T in two parts
+    float at_top, at_top_rest;  // top log2(e) / T in two parts; where T is not usual the halves of log2(e) / T as a double
     bool usual;
     __device__ __forceinline__ void set(float top_, float T)
     {
         top = top_;
         const double c = 1.4426950408889634 / (double)T, ct = c * (double)top;
         per = (float)c;
-        per_rest = isinf(per) ? 0.f : (float)(c - (double)per);
+        per_rest = (float)(c - (double)per);            // (of use where 1 / T is in the range of fp32)
         lowest = top - 45.f * T;                    // 2^40 exp(-45) is below 1
         // The first part has so few bits that it is still exact with an integer down to -66 added.
         usual = fabs(ct) < 1048576.0 && T > 1e-30f && T < 1e30f;
@@ -121,11 +121,15 @@ struct Weight {
         while (usual && fabs(ct) >= 16777216.0 * grain - 66.0) grain *= 2;
         at_top = (float)(rint(ct / grain) * grain);
         at_top_rest = (float)(ct - (double)at_top);
+        if (!usual) {
+            at_top = __int_as_float(__double2hiint(c));
+            at_top_rest = __int_as_float(__double2loint(c));
+        }
     }
     // floor(2^40 exp((l - top) / T)), 2^x of the fraction good to 2^-22
     __device__ __forceinline__ u64 operator()(float l) const
     {
-        if (__builtin_expect(!usual, 0)) return weight_anywhere(l, top, per, per_rest);
+        if (__builtin_expect(!usual, 0)) return weight_anywhere(l, top, __float_as_int(at_top), __float_as_int(at_top_rest));
         l = fmaxf(l, lowest);
         const float t = fmaf(l, per, -at_top) + kNearestInt;
         const float f = fmaf(l, per, -(at_top + (t - kNearestInt))) + fmaf(l, per_rest, -at_top_rest);
@@ -798,7 +802,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     uint32_t least_key = 0;
     if (min_p > 0.f) {
-        least_key = key_of(__double2float_ru((double)r.weight.top + (double)T * log(fmin((double)min_p, 1.0))) + 0.f);
+        const double down = min_p < 1.f ? (double)T * log((double)min_p) : 0.0;         // (not an infinite T times the logarithm of 1)
+        least_key = key_of(__double2float_ru((double)r.weight.top + down) + 0.f);
         if (!filtered) r.make_list(logit_of(least_key));
         filtered = true;
     }
