@@ -63,6 +63,14 @@ cudaError_t launch_after(Kernel kernel, dim3 grid, int threads, size_t smem, boo
     return err != cudaSuccess ? err : cudaGetLastError();
 }
 
+// Lets a kernel (without shared memory of a fixed size) ask for as much as an SM has.  The limit belongs to the process, not to
+// the launch: set to what each call needs, a call of another context on another thread could lower it in between.
+template <typename Kernel>
+cudaError_t allow_shared_memory(Kernel kernel)
+{
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+}
+
 // Per-sequence lengths travel as kernel parameters (the C ABI takes them as
 // host arrays), so a launch needs no host->device copy of its own.
 struct SeqInfo {

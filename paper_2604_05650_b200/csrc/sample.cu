@@ -894,7 +894,7 @@ cudaError_t launch_sample(const SampleParams &params, int rows, bool bf16, bool 
     p.by_cost = rows <= kThreads && rows * p.cluster > 2 * n_sm;
     const size_t smem = sample_smem_bytes(p.vocab, p.cluster);
     const auto kernel = bf16 ? sample_kernel<true> : sample_kernel<false>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = allow_shared_memory(kernel);
     if (e != cudaSuccess) return e;
     if (p.cluster > 8 && (e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};

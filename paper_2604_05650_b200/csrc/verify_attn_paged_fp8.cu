@@ -1342,7 +1342,7 @@ cudaError_t launch_attention(const KernelParams &P, const CUtensorMap &tk, const
 {
     const auto kernel = attn_paged_fp8_kernel<kStreams, kC>;
     const size_t smem = P.sm.total + 1024;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = allow_shared_memory(kernel);
     if (e != cudaSuccess) return e;
     return launch_after(kernel, dim3((unsigned)P.a.n_cta), kThreads, smem, P.a.pdl != 0, stream, launches, P, tk, tv);
 }

@@ -345,13 +345,11 @@ cudaError_t launch_attn_simt(const AttnParams &p, const SeqInfo &seq, cudaStream
     dim3 grid(p.n_split, p.Hkv, p.B);
     cudaError_t err;
     if (p.D == 128) {
-        err = cudaFuncSetAttribute(attn_simt_kernel<128>,
-                                   cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        err = allow_shared_memory(attn_simt_kernel<128>);
         if (err != cudaSuccess) return err;
         attn_simt_kernel<128><<<grid, kThreads, smem, stream>>>(p, seq);
     } else {
-        err = cudaFuncSetAttribute(attn_simt_kernel<64>,
-                                   cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        err = allow_shared_memory(attn_simt_kernel<64>);
         if (err != cudaSuccess) return err;
         attn_simt_kernel<64><<<grid, kThreads, smem, stream>>>(p, seq);
     }

@@ -1915,7 +1915,7 @@ cudaError_t launch_attn_tc(const AttnParams &p, const SeqInfo &seq, cudaStream_t
                                : share <= 4 ? attn_tc_kernel<false, false, 4, true> : attn_tc_kernel<false, false, kMaxChunks, true>)
                   : share <= 2 ? attn_tc_kernel<false, false, 2, false>
                   : share <= 4 ? attn_tc_kernel<false, false, 4, false> : attn_tc_kernel<false, false, kMaxChunks, false>;
-    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t err = allow_shared_memory(kernel);
     if (err != cudaSuccess) return err;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.n_split, p.Hkv, p.B);

@@ -722,7 +722,7 @@ cudaError_t launch_visual_relevance(const RelevanceParams &p, cudaStream_t strea
         !make_rows_map(&md, p.h_draft, p.d, p.K, p.B, NP, P.slabs))
         return cudaErrorInvalidValue;
     const size_t smem = (size_t)P.smem_bytes + 1024;
-    cudaError_t err = cudaFuncSetAttribute(cos_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t err = allow_shared_memory(cos_tc_kernel);
     if (err != cudaSuccess) return err;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)n_cta, 1, 1);
