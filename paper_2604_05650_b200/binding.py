@@ -157,7 +157,8 @@ def _bind_fast(lib) -> None:
     except ImportError:
         _fast = None
         return
-    calls = (lib.lvspec_plan_pages, lib.lvspec_append_paged_fp8, lib.lvspec_verify_attention_paged_fp8, lib.lvspec_sample)
+    calls = (lib.lvspec_set_stream, lib.lvspec_plan_pages, lib.lvspec_append_paged_fp8, lib.lvspec_verify_attention_paged_fp8,
+             lib.lvspec_sample)
     _marshal.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in calls))
     _fast = _marshal
 
@@ -214,7 +215,6 @@ class Context:
             raise LvspecError(st, self._lib.lvspec_last_error(None).decode())
         self._h = h
         self._handle = h.value
-        self._stream = 0
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -235,9 +235,11 @@ class Context:
     def set_stream(self, stream) -> None:
         """``stream``: a raw cudaStream_t address, or an object with ``cuda_stream``."""
         s = getattr(stream, "cuda_stream", stream)
-        if s != self._stream:             # a decoding loop sets the one it has before every call
-            self._check(self._lib.lvspec_set_stream(self._h, ctypes.c_void_p(int(s) if s else 0)))
-            self._stream = s
+        s = int(s) if s else 0
+        if _fast is not None:             # (a decoding loop sets the one it has before every call)
+            st = _fast.set_stream(self._handle, s)
+            return self._check(st) if st else None
+        self._check(self._lib.lvspec_set_stream(self._h, ctypes.c_void_p(s)))
 
     def set_gpu_shared(self, shared: bool = True) -> None:
         """Other work runs on the GPU beside this context's: see ``lvspec_set_gpu_shared``."""

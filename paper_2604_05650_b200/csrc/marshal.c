@@ -9,6 +9,7 @@
 #include "lvspec.h"
 
 static PyObject *name_data_ptr, *name_ctypes, *name_data;
+static __typeof__(&lvspec_set_stream) f_set_stream;
 static __typeof__(&lvspec_plan_pages) f_plan_pages;
 static __typeof__(&lvspec_append_paged_fp8) f_append;
 static __typeof__(&lvspec_verify_attention_paged_fp8) f_attention;
@@ -99,6 +100,13 @@ static int take(Args *a, const void *function, const char *kinds, PyObject *cons
 #define I(k) ((int32_t)a.w[k])
 #define L(k) ((int64_t)a.w[k])
 
+static PyObject *set_stream(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    Args a;
+    if (take(&a, f_set_stream, "pp", args, n)) return NULL;
+    return finish(&a, f_set_stream(P(void *, 0), P(void *, 1)));
+}
 static PyObject *plan_pages(PyObject *self, PyObject *const *args, Py_ssize_t n)
 {
     (void)self;
@@ -147,20 +155,22 @@ static PyObject *sample(PyObject *self, PyObject *const *args, Py_ssize_t n)
     Py_END_ALLOW_THREADS
     return finish(&a, st);
 }
-/* bind(addresses of the four functions, in the order of the methods below) */
+/* bind(addresses of the functions, in the order of the methods below) */
 static PyObject *bind(PyObject *self, PyObject *args)
 {
     (void)self;
-    unsigned long long f[4];
-    if (!PyArg_ParseTuple(args, "KKKK", &f[0], &f[1], &f[2], &f[3])) return NULL;
-    f_plan_pages = (__typeof__(f_plan_pages))(uintptr_t)f[0];
-    f_append = (__typeof__(f_append))(uintptr_t)f[1];
-    f_attention = (__typeof__(f_attention))(uintptr_t)f[2];
-    f_sample = (__typeof__(f_sample))(uintptr_t)f[3];
+    unsigned long long f[5];
+    if (!PyArg_ParseTuple(args, "KKKKK", &f[0], &f[1], &f[2], &f[3], &f[4])) return NULL;
+    f_set_stream = (__typeof__(f_set_stream))(uintptr_t)f[0];
+    f_plan_pages = (__typeof__(f_plan_pages))(uintptr_t)f[1];
+    f_append = (__typeof__(f_append))(uintptr_t)f[2];
+    f_attention = (__typeof__(f_attention))(uintptr_t)f[3];
+    f_sample = (__typeof__(f_sample))(uintptr_t)f[4];
     Py_RETURN_NONE;
 }
 
 static PyMethodDef methods[] = {
+    {"set_stream", (PyCFunction)(void (*)(void))set_stream, METH_FASTCALL, NULL},
     {"plan_pages", (PyCFunction)(void (*)(void))plan_pages, METH_FASTCALL, NULL},
     {"append_paged_fp8", (PyCFunction)(void (*)(void))append_paged_fp8, METH_FASTCALL, NULL},
     {"verify_attention_paged_fp8", (PyCFunction)(void (*)(void))verify_attention_paged_fp8, METH_FASTCALL, NULL},
