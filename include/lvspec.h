@@ -500,7 +500,7 @@ lvspec_status_t lvspec_append_paged_fp8(lvspec_ctx_t *ctx, int32_t n_tokens, int
  * the V scales, vanish from `out` (not from the sums).  q loses nothing down to 2^-10 of the largest finite magnitude among the rows of
  * a KV head; a query that holds a NaN or an infinity gives NaN, the others are not touched by it.  A NaN code of V makes its
  * channel NaN for all queries of the head; in a draft slot (of gamma > 1) it makes those that see the slot NaN in all
- * channels, and does not reach the others.
+ * channels, and does not reach the others.  V scales are taken up to 2^100: larger ones may make `out` infinite where it is not.
  * Scratch: lvspec_attention_paged_fp8_workspace_bytes (for lvspec_reserve ahead of a capture).
  * Errors: as lvspec_verify_attention, and INVALID_ARG for an n_split that is not 0, a cache description out of range, kv_capacity not
  * a whole number of pages, max_kv_len outside 1..kv_capacity or beyond 2^30, batch * n_kv_heads * ceil(max_kv_len / 128) beyond 2^30;

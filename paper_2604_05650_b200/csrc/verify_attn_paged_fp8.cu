@@ -954,10 +954,10 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
                     named_sync(kAll, kSoftmaxThreads);
                     amax = __reduce_max_sync(0xffffffffu, lane < 4 * kGroups ? wmax_s[lane] : 0u);
                 }
-                // the power of two that brings the largest magnitude into [128, 256)
+                // the power of two that brings the largest magnitude into [128, 256); bf16's own range keeps it above 2^-121, and a
+                // largest magnitude below 2^-119 is brought as far as one power goes
                 int shift = 0;
-                if (amax > 0) shift = 7 - ((int)(amax >> 7) - 127);
-                shift = max(-100, min(100, shift));
+                if (amax > 0) shift = min(126, 7 - ((int)(amax >> 7) - 127));
                 const float up = pow2(shift);
                 scale = p.scale_log2 * pow2(-shift);
 #pragma unroll 1
