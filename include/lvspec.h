@@ -171,8 +171,10 @@ int32_t lvspec_attention_splits_fp8(const lvspec_ctx_t *ctx, const lvspec_attn_s
 /* Scratch memory.  A context owns one scratch buffer on its device (split
  * partials of the attention, argmax partials of the acceptance pass, cosines of
  * the relevance score; never results).  A call that needs more than the context
- * holds grows it: that synchronises the context's stream, frees and allocates,
- * and so must not happen inside a CUDA-graph stream capture.  A caller that
+ * holds grows it: that allocates, and so must not happen inside a CUDA-graph
+ * stream capture.  Graphs captured before go on with the buffer they were captured
+ * with, which is freed with the context (the buffer at least doubles when it
+ * grows, so that those kept are smaller than it).  A caller that
  * captures its calls, or that wants every allocation done at start-up, sizes the
  * buffer first:
  *

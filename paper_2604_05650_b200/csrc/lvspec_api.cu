@@ -24,6 +24,8 @@ struct lvspec_ctx {
     uint32_t *plan_ticket = nullptr;  // ticket of the page tables' kernel
     void *scratch = nullptr;          // split partials / argmax partials
     size_t scratch_bytes = 0;
+    void *old_scratch[32] = {};       // earlier, smaller ones: a captured graph may hold any of them
+    int n_old_scratch = 0;
     bool scratch_in_graph = false;    // a call was captured although two waves would not fit: see run_attention
     void *staging = nullptr;          // device copies for the *_host calls
     size_t staging_bytes = 0;
@@ -69,9 +71,11 @@ bool stream_is_capturing(lvspec_ctx *ctx)
     return cs != cudaStreamCaptureStatusNone;
 }
 
-// Grows *buf to at least `want` bytes.  Growing synchronises the stream, frees and
-// allocates: none of that may happen while the stream is being captured, so there the
+// Grows *buf to at least `want` bytes.  Growing allocates (staging memory is freed first, behind
+// a synchronisation): that may not happen while the stream is being captured, so there the
 // call is refused (the capture stays valid) and the caller is told to reserve first.
+// Scratch memory is not freed before the context is: a graph captured earlier goes on using what it
+// was given.  It at least doubles, so that all that is kept is less than what is in use.
 lvspec_status_t ensure(lvspec_ctx *ctx, void **buf, size_t *have, size_t want, bool zero)
 {
     if (want <= *have) return LVSPEC_OK;
@@ -80,7 +84,8 @@ lvspec_status_t ensure(lvspec_ctx *ctx, void **buf, size_t *have, size_t want, b
                     "the call needs " + std::to_string(want) + " bytes of scratch memory, the context holds " +
                         std::to_string(*have) + ", and memory cannot be grown while the stream is being "
                         "captured: call lvspec_reserve (or run the call once) before the capture");
-    if (*buf) {
+    const bool kept = buf == &ctx->scratch;
+    if (*buf && !kept) {
         cudaError_t e = cudaStreamSynchronize(ctx->stream);
         if (e != cudaSuccess) return cuda_fail(ctx, "cudaStreamSynchronize", e);
         cudaFree(*buf);
@@ -88,17 +93,29 @@ lvspec_status_t ensure(lvspec_ctx *ctx, void **buf, size_t *have, size_t want, b
         *have = 0;
     }
     size_t bytes = (want + (size_t(1) << 20) - 1) & ~((size_t(1) << 20) - 1);
-    cudaError_t e = cudaMalloc(buf, bytes);
+    const size_t least = bytes;
+    // (doubling gets past the device's memory before the list ends)
+    if (kept && *buf && ctx->n_old_scratch == (int)(sizeof ctx->old_scratch / sizeof *ctx->old_scratch))
+        return fail(ctx, LVSPEC_ERR_WORKSPACE, "scratch memory has grown too often");
+    if (kept && bytes < 2 * *have) bytes = 2 * *have;
+    void *grown = nullptr;
+    cudaError_t e = cudaMalloc(&grown, bytes);
+    if (e != cudaSuccess && bytes > least) {
+        cudaGetLastError();
+        e = cudaMalloc(&grown, bytes = least);
+    }
     if (e != cudaSuccess) {
         cudaGetLastError();
         return fail(ctx, LVSPEC_ERR_WORKSPACE,
                     "scratch allocation of " + std::to_string(bytes) + " bytes failed");
     }
+    if (*buf) ctx->old_scratch[ctx->n_old_scratch++] = *buf;
+    *buf = grown;
+    *have = bytes;
     if (zero) {
         e = cudaMemsetAsync(*buf, 0, bytes, ctx->stream);
         if (e != cudaSuccess) return cuda_fail(ctx, "cudaMemsetAsync", e);
     }
-    *have = bytes;
     return LVSPEC_OK;
 }
 
@@ -670,6 +687,7 @@ lvspec_status_t lvspec_destroy(lvspec_ctx_t *ctx)
     cudaSetDevice(ctx->device);
     cudaStreamSynchronize(ctx->stream);
     cudaFree(ctx->scratch);
+    for (int i = 0; i < ctx->n_old_scratch; ++i) cudaFree(ctx->old_scratch[i]);
     cudaFree(ctx->staging);
     cudaFree(ctx->status);
     delete ctx;
