@@ -631,7 +631,7 @@ attn_paged_fp8_kernel(const KernelParams P, const __grid_constant__ CUtensorMap 
         bool ok = true;
         while (ok && next_segment(line, walk, seg)) {
             const int32_t *row = p.block_table + (size_t)seg.b * p.pages_per_seq;
-            const int n_live = (seg.len + p.page_size - 1) / p.page_size;
+            const int n_live = (seg.len - 1) / p.page_size + 1;           // (a page may be nearly 2^31 long)
             // 32 entries of the block table at a time, the next 32 on their way
             auto entries = [&](int first) {
                 int e = p.n_pages;                     // outside the pool: reads as zeros
