@@ -74,13 +74,6 @@ __device__ __forceinline__ float2 decode2(uint32_t two)
     return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
 
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 template <int D>
 __global__ void __launch_bounds__(kThreads, 4) append_fp8_kernel(const AppendFp8Params p)
 {

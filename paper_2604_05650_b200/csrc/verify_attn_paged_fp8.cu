@@ -41,13 +41,13 @@
 // Measured, us a call (merge included): 8 heads x 131071 positions x 2 sequences, 20 rows 99 (537 MB, 5.4 TB/s); 16 sequences of
 // 16000 to 32003, 80 rows 238; 32768 positions, 40 rows 28; 8 x 16384 ragged, 7 rows 27; 333 positions 14 (launches and cold code: a
 // CTA's first product is ready 6 us after its lengths).
-#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include <type_traits>
 
 #include "lvspec_internal.h"
 #include "sm100_ptx.cuh"
+#include "tensor_map.h"
 
 namespace lvspec {
 namespace {
@@ -396,12 +396,6 @@ __device__ __forceinline__ float warp_sums(const float *v, int lane)
     return c;
 }
 
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ uint64_t pair(float lo, float hi) { return pack_f32x2(__float_as_uint(lo), __float_as_uint(hi)); }
 __device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16])
 {
@@ -1312,22 +1306,11 @@ __global__ void __launch_bounds__(32 * kMergeWarps) merge_paged_fp8_kernel(const
     if (lane == 0) p.mass[row] = vis * inv;
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // A page pool as [pages][heads][positions][channels]; a box is a tile of one page and head, or all of a shorter page.
 bool make_pool_map(CUtensorMap *map, const uint8_t *pool, const PagedFp8Params &p)
 {
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void *sym = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            return false;
-        fn = reinterpret_cast<EncodeTiledFn>(sym);
-    }
+    const EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)p.D, (cuuint64_t)p.page_size, (cuuint64_t)p.Hkv, (cuuint64_t)p.n_pages};
     const cuuint64_t strides[3] = {(cuuint64_t)p.position_stride, (cuuint64_t)p.head_stride, (cuuint64_t)p.page_stride};
     const cuuint32_t box[4] = {(cuuint32_t)p.D, (cuuint32_t)(p.page_size < kTilePos ? p.page_size : kTilePos), 1, 1};

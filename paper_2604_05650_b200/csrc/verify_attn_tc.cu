@@ -63,7 +63,6 @@
 // head_dim 64: one 64-channel box per K or V tile and four K.Q^T steps; the P.V product
 // keeps its 128 rows, of which the upper 64 read what follows the box in shared memory
 // and fill TMEM lanes nobody reads.
-#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include <cstdio>
@@ -72,6 +71,7 @@
 
 #include "lvspec_internal.h"
 #include "sm100_ptx.cuh"
+#include "tensor_map.h"
 
 #ifdef LVSPEC_TRACE
 cudaError_t lvspec::trace_set_buffer_attention(unsigned long long *device_words)
@@ -1742,25 +1742,6 @@ attn_tc_kernel(const TcParams P, const SeqInfo seq, const __grid_constant__ CUte
 #endif
         }
     }
-}
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
-                                  const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn()
-{
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void *sym = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            return nullptr;
-        fn = reinterpret_cast<EncodeTiledFn>(sym);
-    }
-    return fn;
 }
 
 // A cache as a 4-D tensor [sequences or pages][heads][positions][128 channels] with the

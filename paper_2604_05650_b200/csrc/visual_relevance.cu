@@ -21,11 +21,11 @@
 //                       all cosines), summed in descending order of value
 // The reciprocal norms of H_V's rows come from row_inv_norms_kernel, run once
 // after prefill.
-#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "lvspec_internal.h"
 #include "sm100_ptx.cuh"
+#include "tensor_map.h"
 
 namespace lvspec {
 namespace {
@@ -619,25 +619,6 @@ __global__ void __launch_bounds__(kTopThreads) topn_mean_kernel(const RelevanceP
         for (int o = 16; o > 0; o >>= 1) s2 += __shfl_xor_sync(0xffffffffu, s2, o);
         if (tid == 0) *out = (s2 + (float)need * key_float(prefix)) / (float)n;
     }
-}
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
-                                  const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn()
-{
-    static EncodeTiledFn fn = nullptr;
-    if (!fn) {
-        void *sym = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            return nullptr;
-        fn = reinterpret_cast<EncodeTiledFn>(sym);
-    }
-    return fn;
 }
 
 // [B][rows][d] bf16 as a 4-D tensor (64 channels, rows, slabs of 64 channels, sequences);
