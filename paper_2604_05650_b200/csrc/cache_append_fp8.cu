@@ -17,8 +17,9 @@
 // stay in its registers between the maximum and the codes; rows beyond those (a block of 128 shared by few warps)
 // are read once more, from L2.
 //
-// 21600 tokens of seven prompts, 8 heads of 128, blocks of 32: 35 us for 133 MB, 3.8 TB/s; bound by issue (two thirds of the slots:
-// 100 instructions for eight elements, a third of them the block's maximum and its exchange) and the loads' latency.  The next
+// 21600 tokens of seven prompts, 8 heads of 128, blocks of 32: 35 us for 133 MB, 3.8 TB/s.  Two thirds of the issue slots are taken
+// (100 instructions for eight elements, a third of them the block's maximum and its exchange); the rest goes to the loads' latency, for
+// which a head's exchange between its warps holds up the next head's.  The next
 // head's rows asked for ahead, with 24 warps an SM instead of 32: 37 us.  Two, three, four, eight CTAs for the eight heads: 41,
 // 35, 36, 39 us.
 #include <cuda_fp16.h>

@@ -2,7 +2,8 @@
  * library's function called, without ctypes' conversions.  A pointer is None, an address, an object with
  * data_ptr() (a tensor) or a numpy array; a structure is any object with a buffer of its size.  Returns the status.
  *
- * A call of seventeen arguments, eleven of them tensors: 6.4 us by ctypes, of a call's 10 in all; 1.6 us by this. */
+ * A call of seventeen arguments, eleven of them tensors: 6.4 us by ctypes, of a call's 10 in all; 1.6 us by this.  The stream, which such a
+ * loop sets before each call: 0.44 us and 0.05. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

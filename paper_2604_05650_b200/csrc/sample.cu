@@ -12,14 +12,17 @@
 // A row is read once, by a cluster of up to eight CTAs that keep it in their shared memory (a vocabulary of 152 K is 76 KB
 // each, two CTAs an SM) and pass sums on through distributed shared memory.  A boundary is found without sorting: a histogram over
 // (M - l) in steps of T / 64 or T / 128, then the tokens of the bin that holds the boundary are ranked by comparing all with all (more
-// than 160 by the CTAs together); a bin with more than 1024 tokens (equal or nearly equal logits) is cut into bins of the
-// logits' bit patterns until it fits or holds a single value.  Top-p's bin is chosen by the bins' counts and the weights of their
+// than 160 by the CTAs together); a bin with more than 1024 tokens (equal or nearly equal logits, or the last one, which has no end) is
+// cut into bins of the logits' bit patterns until it fits or holds a single value.  Top-p's bin is chosen by the bins' counts and the weights of their
 // middles; it is ranked together with the bins beside it by exact sums, or put right step by step if it is not among them.  Once a
 // boundary's bin is known each warp lists its tokens up to it, and what follows goes over the lists.
 //
-// Not HBM bounds it but the exchanges (a cluster barrier each, four with top-k, six with top-p) and the passes over shared memory.
+// Not HBM bounds it: with many rows a row's load (a CTA has nothing else to do meanwhile, and an SM one other CTA), and for all the
+// exchanges, a cluster barrier each (two without top-k and top-p, five or six with one of them, seven to nine with both, four
+// more for each cut of a bin), and the passes over shared memory.
 // 128 rows of 152064 in fp32, us: greedy 41, no filter 67, min-p 47, top-k 76, top-p 0.9 145, 0.99 at T = 1.2 248; one row: 6, 9, 8,
-// 13, 22, 38.  With the bins beside the boundary's only, large vocabularies take 10 % less and rows with few tokens a bin, which then
+// 13, 22, 38.  At T = 0.1 top-k 50 ends in the last bin, where most of the row is: with top-p 0.9 198 us and 28 (117 and 20 at
+// T = 0.8).  With the bins beside the boundary's only, large vocabularies take 10 % less and rows with few tokens a bin, which then
 // settle step by step, three times as long (2 rows of 3422, top-k and top-p: 52 us instead of 17).  Sixteen CTAs a row, three an SM,
 // take 50 to 90 % longer with 32 rows or more, and win with few: the barrier's cost against the passes'.
 #include <cfloat>

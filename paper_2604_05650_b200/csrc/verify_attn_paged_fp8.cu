@@ -24,8 +24,9 @@
 // The tiles of a segment (a CTA's share of one sequence and head) go to two streams in turn, each with its own softmax group of
 // four warps, references, sums and accumulators of O, put together when the segment ends: while one group works on a tile the
 // other's products run.  From 97 rows on tensor memory holds one stream, whose two groups share out the columns.  A tile's chain is
-// wait for S^T, pass, vote, P^T there, next K.Q^T: 3700 cycles at 80 rows, 2050 of them the pass (the special-function unit needs
-// 640), and that chain, not HBM, bounds all but the longest launches of few rows.
+// wait for S^T, pass, vote, P^T there, next K.Q^T: at 80 rows 4150 cycles, 930 of them the wait and 2460 the pass (the
+// special-function unit needs 640), the mean over a call's tiles; at 40 rows 2600, 150 and 1800.  That chain, not HBM, bounds all but
+// the longest launches of few rows.
 //
 // The reference exponent of a row is taken from the stream's first tile: its largest probability there becomes 2^6.  It moves (the
 // tile's pass is taken back, a maximum over the lanes, accumulators rescaled, the pass made again) when a score passes 2^14.  fp16 then
@@ -38,9 +39,10 @@
 // different lengths keeps all SMs busy.  Partials of pairs that several CTAs share are merged by a second, small
 // kernel; a pair that one CTA has to itself is finished there.
 //
-// Measured, us a call (merge included): 8 heads x 131071 positions x 2 sequences, 20 rows 99 (537 MB, 5.4 TB/s); 16 sequences of
-// 16000 to 32003, 80 rows 238; 32768 positions, 40 rows 28; 8 x 16384 ragged, 7 rows 27; 333 positions 14 (launches and cold code: a
-// CTA's first product is ready 6 us after its lengths).
+// Measured, us a call (merge included): 8 heads x 131071 positions x 2 sequences, 20 rows 102 (537 MB, 5.3 TB/s); 14 sequences of
+// 16000 to 32003, 80 rows 245 (75 tiles a stream on the busiest SM, 376 000 cycles with the segments' ends, at the 1.8 GHz that the
+// power cap leaves); 32768 positions, 40 rows 28; 8 x 16384 ragged, 7 rows 27; 333 positions 11 (launches and cold code: a CTA's first
+// product is ready 6 us after its lengths).
 #include <cuda_bf16.h>
 
 #include <type_traits>
