@@ -843,11 +843,11 @@ attn_tc_kernel(const TcParams P, const SeqInfo seq, const __grid_constant__ CUte
             amax = 0.f;
 #pragma unroll
             for (int u = 0; u < kSoftmaxWarps; ++u) amax = fmaxf(amax, wmax[u]);
-            // power of two that brings the largest magnitude into [128, 256) (NaN or Inf in q:
-            // no shift; the result is then NaN as it would be with any cache)
+            // power of two that brings the largest magnitude into [128, 256), or, from below 2^-119, as far as one
+            // goes (NaN or Inf in q: no shift; the result is then NaN as it would be with any cache)
             int shift = 0;
             if (amax > 0.f && amax < INFINITY) shift = 7 - ((int)((__float_as_uint(amax) >> 23) & 0xFF) - 127);
-            shift = max(-100, min(100, shift));
+            shift = min(126, shift);
             const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
 #pragma unroll
             for (int u = 0; u < kMine; ++u) {
