@@ -612,6 +612,8 @@ lvspec_status_t lvspec_loose_accept_host(lvspec_ctx_t *ctx, int32_t batch, int32
  *
  *   T <= 0 (or NaN)  the argmax: lowest index among equals, NaN ranks as -inf (and raises
  *                    LVSPEC_DEV_NAN_LOGIT); a row with nothing above -inf gives token 0.  Probability 1.
+ *                    (Any T above 0 is a temperature: a denormal one, or an infinite one, with which all logits above -inf
+ *                    weigh the same.)
  *   otherwise        w_i = exp((l_i - max l) / T).  Tokens are ordered by falling logit, equal ones by
  *                    rising index, and each filter keeps a prefix of that order:
  *     top_k          the first top_k tokens (<= 0 or >= vocab: all)
